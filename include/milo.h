@@ -370,6 +370,93 @@ int milo_moe_w3lr_forward_flags(const milo_half* X, int64_t T, int64_t H, int64_
  */
 int milo_moe_w3lr_routing_status(const void* workspace, void* stream);
 
+/*
+ * ---- Linears, routing and MoE layers beside the 3-bit path: 8-bit integers ----
+ *
+ * W8A8: weights in 8-bit integers with one fp32 scale per output channel, activations quantized inside the call to
+ * 8-bit integers with one fp32 scale per row (token).  Both go by the same rule:
+ *     scale = fp32(max |v| / 127) over the row,   code = round-half-even(v / scale)  of the exact quotient
+ * and the linear is
+ *     Y[m,n] = (sum over k of code_x[m,k] code_w[n,k]) * scale_x[m] * scale_w[n]
+ * with the sum exact in 32-bit integers (whatever the order), its products with the scales in fp32 and one rounding to
+ * the output type.  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale
+ * NaN, so that what is computed from it is NaN and nothing else is touched.
+ * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M <= 2^23 and N K, M K <= 2^40; nothing has to be a
+ * multiple of anything.  Pointers are 16-byte aligned, arrays dense.  These calls need no prepared workspace: theirs is scratch
+ * alone, may hold anything before and after, and keeps nothing between calls; no kernel of theirs waits for another workgroup,
+ * so that they run beside other streams' work and can be captured in a graph.
+ *
+ * Packed weight ("W8 blob"): the codes of an [N x K] weight in blocks of 16 rows by 64 columns, 1024 bytes each, block
+ * (n / 16, k / 64) at ((n / 16) * kb + k / 64) * 1024 with kb = 2 * ceil(K / 128); inside a block the code of row n and column k
+ * lies at ((k % 64) / 16) * 256 + (n % 16) * 16 + k % 16.  Rows and columns that pad to whole blocks are zero.  Behind
+ * the codes: ceil(N / 16) * 16 fp32 scales (0 for the padding).
+ */
+enum milo_dtype { MILO_F32 = 0, MILO_F16 = 1, MILO_BF16 = 2 };
+
+/* Bytes of the W8 blob of an [N x K] weight (0 if the shape is invalid). */
+size_t milo_w8_packed_bytes(int64_t N, int64_t K);
+
+/*
+ * Quantize and pack a weight: W [N x K] row-major of type `dtype` (enum milo_dtype) -> w8, milo_w8_packed_bytes(N, K)
+ * bytes.  Errors: NULL, SHAPE (also an unknown dtype), ALIGN, HIP.
+ */
+int milo_pack_w8(const void* W, int dtype, int64_t N, int64_t K, void* w8, void* stream);
+
+/*
+ * One W8A8 linear: X [M x K] fp16 (bfloat16 with MILO_ACT_BF16 in `flags`), w8 as written by milo_pack_w8, Y [M x N] of
+ * X's type.  workspace: milo_w8a8_gemm_workspace(M, N, K) bytes (0 if the shape is invalid), scratch.
+ * Errors: NULL, SHAPE (also unknown flags), WORKSPACE, ALIGN, HIP.
+ */
+size_t milo_w8a8_gemm_workspace(int64_t M, int64_t N, int64_t K);
+int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t K, const void* w8, unsigned flags, milo_half* Y,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Router of an MoE layer: logits = X Wg^T over E experts, the topk largest of a token (equal ones: lowest id first) and
+ * their softmax weights, in the order of the logits.
+ *   X     [T x H], Wg [E x H]   fp16, or bfloat16 with MILO_ACT_BF16
+ *   ids   out, [T x (topk + n_shared)] int32;  gates  out, the same shape, fp32
+ * The softmax runs over all E experts, with MILO_ROUTE_RENORMALIZE over the chosen ones (their weights then add up to one).
+ * n_shared always-on experts are appended as columns with ids E, E+1, .. and gate 1: the columns milo_moe_w3lr_forward and
+ * milo_moe_w8a8_forward take.  The logits are formed and compared in 64 bits, so the choice does not depend on the order of
+ * the summation.  A NaN logit ranks below every other one (the ids stay distinct and in range) and makes all gates of its token NaN;
+ * so does an infinite largest logit.
+ * Limits: E <= 1024, topk <= min(E, 64), n_shared <= 64, T <= 2^23, H <= 2^20.
+ * Errors: NULL, SHAPE (also unknown flags), ALIGN, HIP.
+ */
+#define MILO_ROUTE_RENORMALIZE 8u
+int milo_moe_route(const milo_half* X, int64_t T, int64_t H, const milo_half* Wg, int E, int topk, int n_shared, unsigned flags,
+                   int32_t* ids, float* gates, void* stream);
+
+/* A SwiGLU expert in W8 blobs (device pointers): w1, w3 are [F x H] (gate, up), w2 is [H x F] (down). */
+typedef struct milo_w8_expert {
+    const void *w1, *w3, *w2;
+} milo_w8_expert;
+
+/* Host-side validation of an expert table before it is copied to the device.  Errors: NULL, SHAPE, ALIGN. */
+int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H, int64_t F);
+
+/*
+ * Top-k routed MoE feed-forward layer over W8A8 experts:
+ *     y_t = sum_j gates[t,j] * lin_w2^e( SiLU(lin_w1^e(x_t)) * lin_w3^e(x_t) ),   e = ids[t,j]
+ * with every lin the W8A8 linear above: a token's activations are quantized once, the SwiGLU output of a (token, expert) pair is
+ * a row of its own, and it is quantized from fp32.  Up to 16 tokens (256 pairs) two launches, reading the weights of the experts
+ * that occur; more tokens are grouped per expert inside the call.
+ *   X  [T x H] fp16, or bfloat16 with MILO_ACT_BF16;  Y the same
+ *   experts      DEVICE array of E entries (a byte copy of a table that passed milo_moe_w8a8_check_experts)
+ *   topk_ids     [T x topk] int32, topk <= E, the ids of one token distinct;  topk_weights  [T x topk] fp32
+ *   status       out, 16 bytes on the DEVICE or NULL: the first word becomes MILO_ERR_ROUTING if an id is outside 0..E-1, else MILO_OK
+ *   workspace    milo_moe_w8a8_workspace(T, H, F, E, topk) bytes (0 if the shape is invalid), scratch
+ * An id outside 0..E-1 contributes nothing; an expert without
+ * tokens is legal, and a token without any gets zeros.  Two runs give bit-identical results.
+ * Limits: as the linear's for [F x H] and [H x F]; the codes of T rows of H and of T topk rows of F within 4 GiB each.
+ * Errors: NULL, SHAPE (also unknown flags), WORKSPACE, ALIGN, HIP.
+ */
+size_t milo_moe_w8a8_workspace(int64_t T, int64_t H, int64_t F, int E, int topk);
+int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, int64_t F, const milo_w8_expert* experts, int E,
+                          const int32_t* topk_ids, const float* topk_weights, int topk, unsigned flags, milo_half* Y,
+                          int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,7 +32,9 @@ EXPORTS = ("milo_status_string", "milo_version", "milo_w3_packed_bytes", "milo_p
            "milo_w3lr_gemm_static", "milo_w3lr_gemm_flags", "milo_lr3_packed_bytes", "milo_pack_lr3",
            "milo_moe_w3lr_check_experts", "milo_moe_w3lr_workspace", "milo_moe_w3lr_forward",
            "milo_moe_w3lr_routing_status", "milo_moe_w3lr_check_experts_flags", "milo_moe_w3lr_forward_flags",
-           "milo_compress_w3lr_workspace", "milo_compress_w3lr")
+           "milo_compress_w3lr_workspace", "milo_compress_w3lr",
+           "milo_w8_packed_bytes", "milo_pack_w8", "milo_w8a8_gemm_workspace", "milo_w8a8_gemm", "milo_moe_route",
+           "milo_moe_w8a8_check_experts", "milo_moe_w8a8_workspace", "milo_moe_w8a8_forward")
 
 
 class MiloError(RuntimeError):
@@ -57,12 +59,18 @@ class Expert(ctypes.Structure):
     _fields_ = [("w1", Weight), ("w3", Weight), ("w2", Weight)]
 
 
+class W8Expert(ctypes.Structure):
+    _fields_ = [("w1", ctypes.c_void_p), ("w3", ctypes.c_void_p), ("w2", ctypes.c_void_p)]
+
+
 _lib = None
 _native = None
 NATIVE_PATH = os.path.join(_HERE, "lib", "_milo_torch.so")
 # the entry points the native marshalling calls (csrc/torch_call.cpp)
 _NATIVE_ENTRIES = ("milo_w3_packed_bytes", "milo_pack_w3", "milo_pack_w3_sym", "milo_w3lr_gemm_workspace",
-                   "milo_w3lr_gemm_flags", "milo_workspace_init", "milo_moe_w3lr_workspace", "milo_moe_w3lr_forward_flags")
+                   "milo_w3lr_gemm_flags", "milo_workspace_init", "milo_moe_w3lr_workspace", "milo_moe_w3lr_forward_flags",
+                   "milo_w8_packed_bytes", "milo_pack_w8", "milo_w8a8_gemm_workspace", "milo_w8a8_gemm", "milo_moe_route",
+                   "milo_moe_w8a8_workspace", "milo_moe_w8a8_forward")
 
 
 def _load_native():
@@ -133,6 +141,22 @@ def bind(path):
     L.milo_moe_w3lr_forward.argtypes = [vp, i64, i64, i64, vp, ci, ci, vp, vp, ci, vp, vp, sz, vp]
     L.milo_moe_w3lr_routing_status.restype = ci
     L.milo_moe_w3lr_routing_status.argtypes = [vp, vp]
+    L.milo_w8_packed_bytes.restype = sz
+    L.milo_w8_packed_bytes.argtypes = [i64, i64]
+    L.milo_pack_w8.restype = ci
+    L.milo_pack_w8.argtypes = [vp, ci, i64, i64, vp, vp]
+    L.milo_w8a8_gemm_workspace.restype = sz
+    L.milo_w8a8_gemm_workspace.argtypes = [i64, i64, i64]
+    L.milo_w8a8_gemm.restype = ci
+    L.milo_w8a8_gemm.argtypes = [vp, i64, i64, i64, vp, ctypes.c_uint, vp, vp, sz, vp]
+    L.milo_moe_route.restype = ci
+    L.milo_moe_route.argtypes = [vp, i64, i64, vp, ci, ci, ci, ctypes.c_uint, vp, vp, vp]
+    L.milo_moe_w8a8_check_experts.restype = ci
+    L.milo_moe_w8a8_check_experts.argtypes = [ctypes.POINTER(W8Expert), ci, i64, i64]
+    L.milo_moe_w8a8_workspace.restype = sz
+    L.milo_moe_w8a8_workspace.argtypes = [i64, i64, i64, ci, ci]
+    L.milo_moe_w8a8_forward.restype = ci
+    L.milo_moe_w8a8_forward.argtypes = [vp, i64, i64, i64, vp, ci, vp, vp, ci, ctypes.c_uint, vp, vp, vp, sz, vp]
     L.entries = _load_native().entries({n: ctypes.cast(getattr(L, n), vp).value for n in _NATIVE_ENTRIES})
     return L
 
@@ -351,3 +375,89 @@ class MoELayer:
 
     def routing_status(self):
         return int(lib().milo_moe_w3lr_routing_status(_ptr(self.last_workspace), _stream()))
+
+
+class W8Weight:
+    """Device buffer of one [N, K] weight in 8-bit integers with a scale per output channel (see include/milo.h)."""
+
+    def __init__(self, N, K, w8):
+        self.N, self.K = int(N), int(K)
+        self.w8 = w8                    # uint8 blob: codes and scales
+
+    def weight_bytes(self):
+        return self.w8.numel()
+
+
+def pack_w8(W):
+    """milo_pack_w8: fp32, fp16 or bf16 CUDA weight [N, K] -> W8Weight."""
+    entries = lib().entries
+    w8 = _native.w8_pack(entries, W)
+    if w8.__class__ is int:
+        raise MiloError(w8, "milo_pack_w8")
+    return W8Weight(W.shape[0], W.shape[1], w8)
+
+
+def w8a8_gemm_workspace_bytes(M, N, K):
+    return int(lib().milo_w8a8_gemm_workspace(M, N, K))
+
+
+def w8a8_gemm(X, w, out=None, workspace=None):
+    """milo_w8a8_gemm: Y = X W^T with X (fp16 or bf16) quantized to 8-bit integers per row and the weight of pack_w8.
+    `workspace`: a uint8 tensor of w8a8_gemm_workspace_bytes (scratch, nothing to prepare); without one the call
+    takes its scratch from PyTorch's allocator."""
+    entries = lib().entries
+    Y = _native.w8_gemm(entries, X, w.w8, w.N, w.K, out, workspace)
+    if Y.__class__ is int:
+        raise MiloError(Y, "milo_w8a8_gemm")
+    return Y
+
+
+def moe_route(X, Wg, topk, renormalize=True, n_shared=0, out=None):
+    """milo_moe_route: logits X Wg^T (X [T, H], Wg [E, H], both fp16 or both bf16) -> (ids int32, gates fp32), both
+    [T, topk + n_shared], as MoELayer.forward and W8MoELayer.forward take them.  `out`: a pair of such tensors."""
+    entries = lib().entries
+    ids, gates = out if out is not None else (None, None)
+    both = _native.route(entries, X, Wg, topk, renormalize, n_shared, ids, gates)
+    if both.__class__ is int:
+        raise MiloError(both, "milo_moe_route")
+    return both
+
+
+class W8MoELayer:
+    """Expert table of one MoE layer whose experts are W8A8 linears: validates on the host, keeps the device copy of the
+    table.  experts: list of (w1, w3, w2) W8Weight triples, w1 and w3 [F, H], w2 [H, F].  One layer takes fp16 and
+    bf16 activations."""
+
+    def __init__(self, experts, H, F):
+        self.H, self.F, self.E = int(H), int(F), len(experts)
+        self.experts = experts                      # keeps the device buffers alive
+        arr = (W8Expert * self.E)()
+        for e, (w1, w3, w2) in enumerate(experts):
+            if (w1.N, w1.K, w3.N, w3.K, w2.N, w2.K) != (self.F, self.H, self.F, self.H, self.H, self.F):
+                raise ValueError(f"expert {e}: w1 and w3 must be [F, H], w2 [H, F]")
+            arr[e] = W8Expert(w1.w8.data_ptr(), w3.w8.data_ptr(), w2.w8.data_ptr())
+        _check(lib().milo_moe_w8a8_check_experts(arr, self.E, self.H, self.F), "milo_moe_w8a8_check_experts")
+        device = experts[0][0].w8.device
+        if any(w.w8.device != device for triple in experts for w in triple):
+            raise ValueError("all experts must be on one device")
+        self.table = torch.from_numpy(np.frombuffer(bytes(arr), dtype=np.uint8).copy()).to(device)
+        self.last_status = None
+
+    def workspace_bytes(self, T, topk):
+        return int(lib().milo_moe_w8a8_workspace(T, self.H, self.F, self.E, topk))
+
+    def forward(self, X, ids, gates, out=None, workspace=None):
+        """`workspace`: a uint8 tensor of workspace_bytes (scratch, nothing to prepare); without one the call takes its
+        scratch from PyTorch's allocator."""
+        entries = lib().entries
+        status = torch.empty(4, dtype=torch.int32, device=self.table.device)
+        Y = _native.w8_moe(entries, X, ids, gates, self.table, self.H, self.F, self.E, out, status, workspace)
+        if Y.__class__ is int:
+            raise MiloError(Y, "milo_moe_w8a8_forward")
+        self.last_status = status
+        return Y
+
+    def routing_status(self):
+        """0, or MILO_ERR_ROUTING (6) if the last forward met an expert id outside 0..E-1 (such a pair contributes
+        nothing).  Waits for the current stream."""
+        return int(self.last_status[0].item())

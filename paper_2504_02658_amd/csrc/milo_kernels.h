@@ -24,6 +24,23 @@ struct TileDesc {
     int32_t pad;
 };
 
+// Grouping of routed pairs by expert (moe.hip).
+struct RouteArgs {
+    const int32_t* ids;     // [P] expert id per (token, slot) pair, pair index p = t*topk + j
+    int32_t P;
+    int32_t E;
+    int32_t bm;             // rows per M-tile
+    int32_t topk;
+    int32_t* sorted;        // [P] pair indices grouped by expert, original order inside a group
+    int32_t* sorted_token;  // [P] token of each sorted pair (pair / topk)
+    TileDesc* tiles;
+    int32_t* header;        // [0] routing status, [1] number of tiles, [3] wait status (a wait gave up)
+    uint32_t* flags;        // per-tile control words of the GEMM kernels, cleared here
+    int32_t n_flags;
+    int32_t max_tiles;      // slots of the tile list: ceil(P / bm) + E
+};
+int launch_pair_groups(const RouteArgs& a, hipStream_t stream);     // route_kernel, the slots as they are
+
 // Row-space conventions of the tiled kernel.
 //   Ungrouped (tiles == nullptr): tile y covers rows [y*BM, min(M, (y+1)*BM)), weights = w[].
 //   Grouped: tile y = tiles[y] if y < *n_tiles (else the workgroup exits); the weights are

@@ -23,21 +23,6 @@ namespace milo {
 
 constexpr int kRouteThreads = 1024;
 
-struct RouteArgs {
-    const int32_t* ids;     // [P] expert id per (token, slot) pair, pair index p = t*topk + j
-    int32_t P;
-    int32_t E;
-    int32_t bm;             // rows per M-tile
-    int32_t topk;
-    int32_t* sorted;        // [P] pair indices grouped by expert, original order inside a group
-    int32_t* sorted_token;  // [P] token of each sorted pair (pair / topk)
-    TileDesc* tiles;
-    int32_t* header;        // [0] routing status, [1] number of tiles, [3] wait status (a wait gave up)
-    uint32_t* flags;        // per-tile control words of the GEMM kernels, cleared here
-    int32_t n_flags;
-    int32_t max_tiles;      // slots of the tile list: ceil(P / bm) + E
-};
-
 // One workgroup per expert; no workgroup depends on another one, so a single launch suffices.
 // A wave owns a contiguous range of the pairs, 256 of them per step (a lane four neighbours, one 16-byte load) and eight steps
 // of them in registers, and finds its expert's pairs with one ballot per lane slot: the stable position of a pair inside
@@ -635,6 +620,11 @@ static int check_weight(const milo_w3lr_weight& w, int64_t N, int64_t K) {
     if (!aligned16(w.q3) || !aligned16(w.U) || !aligned16(w.V))
         return MILO_ERR_ALIGN;
     return MILO_OK;
+}
+
+int launch_pair_groups(const RouteArgs& a, hipStream_t stream) {
+    route_kernel<<<dim3((unsigned)a.E), dim3(kRouteThreads), 0, stream>>>(a);
+    return launch_status();
 }
 
 }  // namespace milo

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -27,10 +28,19 @@ struct Entries {
     decltype(&milo_workspace_init) workspace_init;
     decltype(&milo_moe_w3lr_workspace) moe_workspace;
     decltype(&milo_moe_w3lr_forward_flags) moe;
+    decltype(&milo_w8_packed_bytes) w8_bytes;
+    decltype(&milo_pack_w8) w8_pack;
+    decltype(&milo_w8a8_gemm_workspace) w8_workspace;
+    decltype(&milo_w8a8_gemm) w8_gemm;
+    decltype(&milo_moe_route) route;
+    decltype(&milo_moe_w8a8_workspace) w8_moe_workspace;
+    decltype(&milo_moe_w8a8_forward) w8_moe;
 };
 constexpr const char* kEntryNames[] = {"milo_w3_packed_bytes", "milo_pack_w3", "milo_pack_w3_sym",
                                        "milo_w3lr_gemm_workspace", "milo_w3lr_gemm_flags", "milo_workspace_init",
-                                       "milo_moe_w3lr_workspace", "milo_moe_w3lr_forward_flags"};
+                                       "milo_moe_w3lr_workspace", "milo_moe_w3lr_forward_flags",
+                                       "milo_w8_packed_bytes", "milo_pack_w8", "milo_w8a8_gemm_workspace", "milo_w8a8_gemm",
+                                       "milo_moe_route", "milo_moe_w8a8_workspace", "milo_moe_w8a8_forward"};
 constexpr size_t kEntries = sizeof(kEntryNames) / sizeof(kEntryNames[0]);
 static_assert(sizeof(Entries) == kEntries * sizeof(void*), "one address per entry point");
 
@@ -224,11 +234,182 @@ PyObject* py_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- the 8-bit path: tensors of any device, whose current stream the call takes ----
+
+// A contiguous matrix of type `dt` (and, where `like` is given, on its device), or nullptr with an error set.
+const at::Tensor* matrix(PyObject* o, at::ScalarType dt, const char* name, const at::Tensor* like) {
+    const at::Tensor* t = device_tensor(o, dt, name);
+    if (!t) return nullptr;
+    if (t->dim() != 2) {
+        PyErr_Format(PyExc_ValueError, "%s must have two dimensions", name);
+        return nullptr;
+    }
+    if (like && t->device() != like->device()) {
+        PyErr_Format(PyExc_ValueError, "%s must be on the device of the other tensors", name);
+        return nullptr;
+    }
+    return t;
+}
+// fp16 or bf16 activations.
+const at::Tensor* activations(PyObject* o, bool* bf) {
+    *bf = THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kBFloat16;
+    return matrix(o, *bf ? at::kBFloat16 : at::kHalf, "X", nullptr);
+}
+// A byte buffer on `like`'s device (a packed weight, an expert table).
+const at::Tensor* bytes_on(PyObject* o, const char* name, const at::Tensor& like) {
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.scalar_type() == at::kByte && t.is_contiguous() && t.device() == like.device()) return &t;
+    }
+    PyErr_Format(PyExc_TypeError, "%s must be a contiguous tensor of torch.uint8 on the device of X", name);
+    return nullptr;
+}
+// The output: the caller's, which has to be a contiguous [rows x cols] of type `dt` on X's device, or a new one.
+bool output(PyObject* o, at::ScalarType dt, int64_t rows, int64_t cols, const at::Tensor& X, const char* name, at::Tensor* out) {
+    if (o == Py_None) {
+        *out = at::empty({rows, cols}, X.options().dtype(dt));
+        return true;
+    }
+    const at::Tensor* t = matrix(o, dt, name, &X);
+    if (!t) return false;
+    if (t->size(0) != rows || t->size(1) != cols) {
+        PyErr_Format(PyExc_ValueError, "%s must be [%lld, %lld]", name, (long long)rows, (long long)cols);
+        return false;
+    }
+    *out = *t;
+    return true;
+}
+// Scratch of `need` bytes: the caller's buffer, whatever it has, or a new one from the allocator (on the current stream, so that
+// neither another stream's call nor another captured graph's shares it).
+bool scratch(PyObject* o, size_t need, const at::Tensor& X, at::Tensor* ws) {
+    if (o == Py_None) {
+        *ws = at::empty({(int64_t)(need > 16 ? need : 16)}, X.options().dtype(at::kByte));
+        return true;
+    }
+    const at::Tensor* t = bytes_on(o, "workspace", X);
+    if (t) *ws = *t;
+    return t != nullptr;
+}
+
+// w8_pack(entries, W): the blob of W, or a non-zero status.
+PyObject* py_w8_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 2) return PyErr_Format(PyExc_TypeError, "w8_pack takes 2 arguments");
+    return guarded([&]() -> PyObject* {
+        const Entries* e = entries_of(a[0]);
+        if (!e) return nullptr;
+        const at::ScalarType have = THPVariable_Check(a[1]) ? THPVariable_Unpack(a[1]).scalar_type() : at::kFloat;
+        const at::ScalarType dt = have == at::kHalf || have == at::kBFloat16 ? have : at::kFloat;
+        const at::Tensor* W = matrix(a[1], dt, "W", nullptr);
+        if (!W) return nullptr;
+        const c10::DeviceGuard device(W->device());
+        const int64_t N = W->size(0), K = W->size(1);
+        const size_t bytes = e->w8_bytes(N, K);
+        at::Tensor blob = at::empty({(int64_t)(bytes > 16 ? bytes : 16)}, W->options().dtype(at::kByte));
+        const int st = e->w8_pack(W->data_ptr(), dt == at::kHalf ? MILO_F16 : dt == at::kBFloat16 ? MILO_BF16 : MILO_F32, N, K, blob.data_ptr(),
+                                  current_stream());
+        if (st != MILO_OK) return status_object(st);
+        return THPVariable_Wrap(std::move(blob));
+    });
+}
+
+// w8_gemm(entries, X, blob, N, K, out, workspace): the output tensor, or a non-zero status.
+PyObject* py_w8_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "w8_gemm takes 7 arguments");
+    return guarded([&]() -> PyObject* {
+        const Entries* e = entries_of(a[0]);
+        if (!e) return nullptr;
+        bool bf;
+        const at::Tensor* X = activations(a[1], &bf);
+        const at::Tensor* blob = X ? bytes_on(a[2], "the packed weight", *X) : nullptr;
+        int64_t N, K;
+        if (!blob || !whole(a[3], &N) || !whole(a[4], &K)) return nullptr;
+        const int64_t M = X->size(0);
+        if (X->size(1) != K) return PyErr_Format(PyExc_ValueError, "X and weight disagree on K");
+        if ((size_t)blob->numel() < e->w8_bytes(N, K)) return PyErr_Format(PyExc_ValueError, "the packed weight is smaller than its shape says");
+        const c10::DeviceGuard device(X->device());
+        at::Tensor Y, ws;
+        if (!output(a[5], X->scalar_type(), M, N, *X, "out", &Y) || !scratch(a[6], e->w8_workspace(M, N, K), *X, &ws)) return nullptr;
+        const int st = e->w8_gemm(static_cast<const milo_half*>(X->data_ptr()), M, N, K, blob->data_ptr(), bf ? MILO_ACT_BF16 : 0u,
+                                  static_cast<milo_half*>(Y.data_ptr()), ws.data_ptr(), (size_t)ws.numel(), current_stream());
+        if (st != MILO_OK) return status_object(st);
+        return THPVariable_Wrap(std::move(Y));
+    });
+}
+
+// route(entries, X, Wg, topk, renormalize, n_shared, ids, gates): (ids, gates), or a non-zero status.
+PyObject* py_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "route takes 8 arguments");
+    return guarded([&]() -> PyObject* {
+        const Entries* e = entries_of(a[0]);
+        if (!e) return nullptr;
+        bool bf;
+        const at::Tensor* X = activations(a[1], &bf);
+        const at::Tensor* Wg = X ? matrix(a[2], X->scalar_type(), "Wg", X) : nullptr;
+        int64_t topk, shared;
+        if (!Wg || !whole(a[3], &topk) || !whole(a[5], &shared)) return nullptr;
+        const int renormalize = PyObject_IsTrue(a[4]);
+        if (renormalize < 0) return nullptr;
+        const int64_t T = X->size(0), H = X->size(1), E = Wg->size(0);
+        if (Wg->size(1) != H) return PyErr_Format(PyExc_ValueError, "X and Wg disagree on H");
+        if (topk < 1 || topk > E || E > INT32_MAX || shared < 0 || shared > INT32_MAX) return status_object(MILO_ERR_SHAPE);
+        const c10::DeviceGuard device(X->device());
+        at::Tensor ids, gates;
+        if (!output(a[6], at::kInt, T, topk + shared, *X, "ids", &ids) || !output(a[7], at::kFloat, T, topk + shared, *X, "gates", &gates)) return nullptr;
+        const int st = e->route(static_cast<const milo_half*>(X->data_ptr()), T, H, static_cast<const milo_half*>(Wg->data_ptr()), (int)E, (int)topk,
+                                (int)shared, (bf ? MILO_ACT_BF16 : 0u) | (renormalize ? MILO_ROUTE_RENORMALIZE : 0u),
+                                static_cast<int32_t*>(ids.data_ptr()), static_cast<float*>(gates.data_ptr()), current_stream());
+        if (st != MILO_OK) return status_object(st);
+        PyObject* const i = THPVariable_Wrap(std::move(ids));
+        PyObject* const g = i ? THPVariable_Wrap(std::move(gates)) : nullptr;
+        PyObject* const both = g ? PyTuple_Pack(2, i, g) : nullptr;
+        Py_XDECREF(i);
+        Py_XDECREF(g);
+        return both;
+    });
+}
+
+// w8_moe(entries, X, ids, gates, table, H, F, E, out, status, workspace): the output tensor, or a non-zero status.
+PyObject* py_w8_moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 11) return PyErr_Format(PyExc_TypeError, "w8_moe takes 11 arguments");
+    return guarded([&]() -> PyObject* {
+        const Entries* e = entries_of(a[0]);
+        if (!e) return nullptr;
+        bool bf;
+        const at::Tensor* X = activations(a[1], &bf);
+        const at::Tensor* ids = X ? matrix(a[2], at::kInt, "ids", X) : nullptr;
+        const at::Tensor* gates = ids ? matrix(a[3], at::kFloat, "gates", X) : nullptr;
+        const at::Tensor* table = gates ? bytes_on(a[4], "the expert table", *X) : nullptr;
+        int64_t H, F, E;
+        if (!table || !whole(a[5], &H) || !whole(a[6], &F) || !whole(a[7], &E)) return nullptr;
+        const int64_t T = X->size(0), topk = ids->size(1);
+        if (X->size(1) != H) return PyErr_Format(PyExc_ValueError, "X must have H columns");
+        if (ids->size(0) != T || gates->size(0) != T || gates->size(1) != topk)
+            return PyErr_Format(PyExc_ValueError, "ids and gates must have the same shape, with a row for every row of X");
+        if (topk > INT32_MAX || E > INT32_MAX || (size_t)table->numel() < (size_t)E * sizeof(milo_w8_expert)) return status_object(MILO_ERR_SHAPE);
+        const c10::DeviceGuard device(X->device());
+        at::Tensor Y, ws;
+        if (!output(a[8], X->scalar_type(), T, H, *X, "out", &Y) || !scratch(a[10], e->w8_moe_workspace(T, H, F, (int)E, (int)topk), *X, &ws)) return nullptr;
+        const at::Tensor* status = device_tensor(a[9], at::kInt, "status");
+        if (!status) return nullptr;
+        if (status->numel() < 4 || status->device() != X->device()) return PyErr_Format(PyExc_ValueError, "status must have four words on the device of X");
+        const int st = e->w8_moe(static_cast<const milo_half*>(X->data_ptr()), T, H, F, static_cast<const milo_w8_expert*>(table->data_ptr()), (int)E,
+                                 static_cast<const int32_t*>(ids->data_ptr()), static_cast<const float*>(gates->data_ptr()), (int)topk,
+                                 bf ? MILO_ACT_BF16 : 0u, static_cast<milo_half*>(Y.data_ptr()), static_cast<int32_t*>(status->data_ptr()),
+                                 ws.data_ptr(), (size_t)ws.numel(), current_stream());
+        if (st != MILO_OK) return status_object(st);
+        return THPVariable_Wrap(std::move(Y));
+    });
+}
+
 PyMethodDef kMethods[] = {
     {"entries", py_entries, METH_O, "addresses of a loaded library's entry points"},
     {"gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_gemm)), METH_FASTCALL, "milo_w3lr_gemm_flags on tensors"},
     {"moe", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_moe)), METH_FASTCALL, "milo_moe_w3lr_forward_flags on tensors"},
     {"pack", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_pack)), METH_FASTCALL, "milo_pack_w3(_sym) on tensors"},
+    {"w8_pack", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_w8_pack)), METH_FASTCALL, "milo_pack_w8 on tensors"},
+    {"w8_gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_w8_gemm)), METH_FASTCALL, "milo_w8a8_gemm on tensors"},
+    {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_route)), METH_FASTCALL, "milo_moe_route on tensors"},
+    {"w8_moe", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_w8_moe)), METH_FASTCALL, "milo_moe_w8a8_forward on tensors"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_milo_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

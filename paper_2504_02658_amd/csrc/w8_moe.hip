@@ -1,0 +1,406 @@
+// milo_moe_w8a8_forward: top-k routed SwiGLU experts over 8-bit integer linears.
+//
+// Up to kFewTokens tokens, two launches, both bound by the bytes of the weights of the experts that some token goes to:
+//   few_up    a workgroup owns 16 of the F features of one expert (gate and up): it finds the expert's tokens in the ids,
+//             quantizes their activations, multiplies, and writes H = SiLU(gate) * up with the largest magnitude of
+//             its 16 features per row
+//   few_down  a workgroup owns 16 of the H features of the output and walks all experts: it quantizes the rows of H and
+//             adds each expert's product, weighted, to the tokens' sums, so that nothing is left to combine
+// More tokens: the activations' rows are quantized once, pairs grouped per expert (route_kernel of moe.hip), gate and up as one
+// grouped product over the tiles, the SwiGLU rows quantized, the grouped down projection, and the sum over a token's pairs.
+#include "milo_host.h"
+#include "w8_kernels.h"
+
+namespace milo {
+
+constexpr int kFewTokens = 16, kFewMaxPairs = 256;
+constexpr int kFewUpThreads = 256, kFewDownThreads = 512;
+constexpr int kFewUpLds = 48 * 1024, kFewDownLds = 48 * 1024;       // most bytes of codes that a workgroup holds at once
+
+struct W8FewArgs {
+    const void* X;
+    int T, topk, E;
+    int64_t H, F;
+    const milo_w8_expert* experts;
+    const int32_t* ids;
+    const float* gates;
+    int32_t* status;        // routing status
+    float* h;               // [pairs x F]
+    uint32_t* tops;         // [pairs x ceil(F/16)] largest magnitude of 16 features of H, fp32 bits
+    uint16_t* Y;
+};
+
+// The experts that occur in the ids, in the order of their first occurrence: their number, and in list[i] the i-th
+// one's id for all i below it.  All threads of the workgroup take part; s_ids receives the ids, -1 for one out of range.
+template <int THREADS>
+__device__ __forceinline__ int distinct_experts(const W8FewArgs& a, int32_t* s_ids, int32_t* s_list, int32_t* s_count, bool* bad) {
+    static_assert(THREADS >= kFewMaxPairs, "a thread per pair");
+    const int tid = threadIdx.x, P = a.T * a.topk;
+    int id = -1;
+    if (tid < P) {
+        id = a.ids[tid];
+        if (id < 0 || id >= a.E) id = -1;
+    }
+    if (tid < kFewMaxPairs) s_ids[tid] = id;
+    *bad = __syncthreads_or(tid < P && id < 0) != 0;
+    bool first = id >= 0;
+    for (int q = 0; q < P; ++q) first = first && !(q < tid && s_ids[q] == id);
+    const unsigned long long m = __builtin_amdgcn_ballot_w64(first);
+    if ((tid & 63) == 0) s_count[tid >> 6] = __popcll(m);
+    __syncthreads();
+    int at = __popcll(m & ((1ull << (tid & 63)) - 1ull)), total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        at += w < (tid >> 6) ? s_count[w] : 0;
+        total += s_count[w];
+    }
+    if (first) s_list[at] = id;
+    __syncthreads();
+    return total;
+}
+// The slot of token t that expert e is in (its first, if the caller repeats one), or -1.
+__device__ __forceinline__ int slot_of(const int32_t* s_ids, int topk, int t, int e) {
+    int found = -1;
+    for (int j = topk - 1; j >= 0; --j) found = s_ids[t * topk + j] == e ? j : found;
+    return found;
+}
+
+// Codes in LDS: 64-column unit u of token t, piece c of 16 columns, at ((u * 4 + c) * T + t) * 16.
+template <int IN>
+__global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArgs a, int lds_units) {
+    constexpr int NW = kFewUpThreads / 64;
+    __shared__ int32_t s_ids[kFewMaxPairs], s_list[kFewMaxPairs], s_count[NW];
+    __shared__ int32_t s_slot[kFewTokens];
+    __shared__ RowStep s_step[kFewTokens];
+    __shared__ i32x4 s_part[2][NW][64];
+    extern __shared__ __attribute__((aligned(16))) unsigned char codes[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int slot = blockIdx.y;
+    bool bad;
+    const int total = distinct_experts<kFewUpThreads>(a, s_ids, s_list, s_count, &bad);
+    if (blockIdx.x == 0 && slot == 0 && tid == 0) a.status[0] = bad ? MILO_ERR_ROUTING : MILO_OK;
+    if (slot >= total) return;
+    const int e = __builtin_amdgcn_readfirstlane(s_list[slot]);
+    if (tid < kFewTokens) s_slot[tid] = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
+    __syncthreads();
+    const char* const X = reinterpret_cast<const char*>(a.X);
+    const int kb = (int)w8_kblocks(a.H);
+    for (int t = wave; t < a.T; t += NW) {
+        if (s_slot[t] < 0) continue;
+        uint32_t top = 0u;
+        for (int p = lane; p < kb * 4; p += 64) top = raw_top<IN>(load16<IN>(X + t * a.H * 2, (int64_t)p * 16, a.H), top);
+        top = wave_max(top);
+        if (lane == 0) s_step[t] = row_step(top);
+    }
+    const milo_w8_expert& ex = a.experts[e];
+    const int64_t wskip = (int64_t)blockIdx.x * kb * 1024;
+    const u32x4* const w1 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(ex.w1) + wskip) + lane;
+    const u32x4* const w3 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(ex.w3) + wskip) + lane;
+    i32x4 acc1 = {0, 0, 0, 0}, acc3 = {0, 0, 0, 0};
+    const int m = lane & 15, c16 = lane >> 4;
+    const bool mine = m < a.T && s_slot[m] >= 0;
+    for (int u0 = 0; u0 < kb; u0 += lds_units) {
+        const int units = kb - u0 < lds_units ? kb - u0 : lds_units;
+        __syncthreads();
+        for (int i = tid; i < units * 4 * a.T; i += kFewUpThreads) {
+            const int t = i % a.T, p = i / a.T;
+            if (s_slot[t] < 0) continue;
+            float v[16];
+            raw_values<IN>(load16<IN>(X + t * a.H * 2, (int64_t)(u0 * 4 + p) * 16, a.H), v);
+            *reinterpret_cast<u32x4*>(codes + i * 16) = row_codes16(v, s_step[t]);
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int u = wave; u < units; u += NW) {
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (mine) x = *reinterpret_cast<const u32x4*>(codes + ((u * 4 + c16) * a.T + m) * 16);
+            acc1 = mfma16_i8(w1[(int64_t)(u0 + u) * 64], x, acc1);
+            acc3 = mfma16_i8(w3[(int64_t)(u0 + u) * 64], x, acc3);
+        }
+    }
+    s_part[0][wave][lane] = acc1;
+    s_part[1][wave][lane] = acc3;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 1; i < NW; ++i) {
+        acc1 += s_part[0][i][lane];
+        acc3 += s_part[1][i][lane];
+    }
+    const int64_t n = (int64_t)blockIdx.x * 16 + c16 * 4;
+    uint32_t top = 0u;
+    const int64_t row = mine ? m * a.topk + s_slot[m] : 0;
+    if (mine) {
+        const float* const sw1 = w8_scales(ex.w1, a.F, a.H) + n;
+        const float* const sw3 = w8_scales(ex.w3, a.F, a.H) + n;
+        const float sx = s_step[m].s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (n + i >= a.F) continue;
+            const float v = silu_times((float)acc1[i] * sx * sw1[i], (float)acc3[i] * sx * sw3[i]);
+            a.h[row * a.F + n + i] = v;
+            const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+            top = b > top ? b : top;
+        }
+    }
+#pragma unroll
+    for (int d = 16; d <= 32; d <<= 1) {
+        const uint32_t o = __shfl_xor(top, d, 64);
+        top = o > top ? o : top;
+    }
+    if (mine && c16 == 0) a.tops[row * ((a.F + 15) / 16) + blockIdx.x] = top;
+}
+
+template <bool BF>
+__global__ __launch_bounds__(kFewDownThreads) void w8_few_down_kernel(const W8FewArgs a, int lds_units) {
+    constexpr int NW = kFewDownThreads / 64;
+    __shared__ int32_t s_ids[kFewMaxPairs], s_list[kFewMaxPairs], s_count[NW];
+    __shared__ int32_t s_slot[kFewTokens];
+    __shared__ RowStep s_step[kFewTokens];
+    __shared__ float s_gate[kFewTokens];
+    __shared__ f32x4 s_part[NW][64];
+    extern __shared__ __attribute__((aligned(16))) unsigned char codes[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    bool bad;
+    const int total = distinct_experts<kFewDownThreads>(a, s_ids, s_list, s_count, &bad);
+    const int kb = (int)w8_kblocks(a.F), nt = (int)((a.F + 15) / 16);
+    const int m = lane & 15, c16 = lane >> 4;
+    const int64_t n = (int64_t)blockIdx.x * 16 + c16 * 4;
+    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < total; ++s) {
+        const int e = __builtin_amdgcn_readfirstlane(s_list[s]);
+        __syncthreads();
+        if (tid < kFewTokens) {
+            const int j = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
+            s_slot[tid] = j;
+            float g = 0.0f;
+            if (j >= 0)
+                for (int i = 0; i < a.topk; ++i) g += s_ids[tid * a.topk + i] == e ? a.gates[tid * a.topk + i] : 0.0f;
+            s_gate[tid] = g;
+        }
+        __syncthreads();
+        for (int t = wave; t < a.T; t += NW) {
+            if (s_slot[t] < 0) continue;
+            uint32_t top = 0u;
+            const uint32_t* const tops = a.tops + (int64_t)(t * a.topk + s_slot[t]) * nt;
+            for (int i = lane; i < nt; i += 64) top = tops[i] > top ? tops[i] : top;
+            top = wave_max(top);
+            if (lane == 0) s_step[t] = row_step(top);
+        }
+        const void* const w2 = a.experts[e].w2;
+        const u32x4* const w = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(w2) + (int64_t)blockIdx.x * kb * 1024) + lane;
+        i32x4 acc = {0, 0, 0, 0};
+        const bool mine = m < a.T && s_slot[m] >= 0;
+        for (int u0 = 0; u0 < kb; u0 += lds_units) {
+            const int units = kb - u0 < lds_units ? kb - u0 : lds_units;
+            __syncthreads();
+            for (int i = tid; i < units * 4 * a.T; i += kFewDownThreads) {
+                const int t = i % a.T, p = i / a.T;
+                if (s_slot[t] < 0) continue;
+                float v[16];
+                raw_values<W8_F32>(load16<W8_F32>(a.h + (int64_t)(t * a.topk + s_slot[t]) * a.F, (int64_t)(u0 * 4 + p) * 16, a.F), v);
+                *reinterpret_cast<u32x4*>(codes + i * 16) = row_codes16(v, s_step[t]);
+            }
+            __syncthreads();
+#pragma unroll 4
+            for (int u = wave; u < units; u += NW) {
+                u32x4 x = {0u, 0u, 0u, 0u};
+                if (mine) x = *reinterpret_cast<const u32x4*>(codes + ((u * 4 + c16) * a.T + m) * 16);
+                acc = mfma16_i8(w[(int64_t)(u0 + u) * 64], x, acc);
+            }
+        }
+        if (mine && n < a.H) {
+            const float* const sw = w8_scales(w2, a.H, a.F) + n;        // (there are scales for whole blocks of 16)
+            const float f = s_step[m].s;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * f * sw[i] * s_gate[m];
+        }
+    }
+    s_part[wave][lane] = y;
+    __syncthreads();
+    if (wave != 0 || m >= a.T || n >= a.H) return;
+#pragma unroll
+    for (int i = 1; i < NW; ++i) y += s_part[i][lane];
+    const float v[4] = {y[0], y[1], y[2], y[3]};
+    store4<BF>(a.Y + m * a.H + n, v, (int)(a.H - n < 4 ? a.H - n : 4), (a.H & 3) == 0);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Y = sum over a token's pairs of their rows of O, in slot order; a pair whose id is out of range has none.
+template <bool BF>
+__global__ __launch_bounds__(256) void w8_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ ids, int topk, int E, int64_t H,
+                                                         uint16_t* __restrict__ Y) {
+    const int64_t t = blockIdx.x;
+    for (int64_t h = (int64_t)threadIdx.x * 4; h < H; h += 1024) {
+        const int left = (int)(H - h < 4 ? H - h : 4);
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < topk; ++j) {
+            const int64_t p = t * topk + j;
+            if ((uint32_t)ids[p] >= (uint32_t)E) continue;
+            const float* const o = O + p * H + h;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) v[i] += o[i];
+        }
+        store4<BF>(Y + t * H + h, v, left, (H & 3) == 0);
+    }
+}
+
+// Workspace of a forward.
+struct W8MoeLayout {
+    bool few;
+    int bm, max_tiles;
+    size_t off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
+};
+static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8MoeLayout* L) {
+    if (T < 1 || E < 1 || E > 65536 || topk < 1 || topk > E) return false;
+    if (!w8_shape_ok(F, H) || !w8_shape_ok(H, F)) return false;
+    if (T > (int64_t(1) << 30) / topk) return false;
+    const int64_t P = T * topk, hb = w8_kblocks(H) * 64, fb = w8_kblocks(F) * 64;
+    // rows of codes are addressed with 32-bit offsets
+    if (T * hb >= 0xFFFF0000ll || P * fb >= 0xFFFF0000ll) return false;
+    size_t off = 256;
+    L->off_status = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, 256);
+        return at;
+    };
+    L->few = T <= kFewTokens && P <= kFewMaxPairs;
+    L->off_h = take((size_t)P * F * 4);
+    if (L->few) {
+        L->off_tops = take((size_t)P * ((F + 15) / 16) * 4);
+    } else {
+        L->bm = P >= 192 * (int64_t)E ? 256 : 128;
+        L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
+        L->off_xq = take((size_t)(T * hb));
+        L->off_xs = take((size_t)T * 4);
+        L->off_sorted = take((size_t)P * 4);
+        L->off_token = take((size_t)P * 4);
+        L->off_tiles = take((size_t)L->max_tiles * sizeof(TileDesc));
+        L->off_hq = take((size_t)(P * fb));
+        L->off_hs = take((size_t)P * 4);
+        L->off_o = take((size_t)P * H * 4);
+    }
+    L->total = off;
+    return true;
+}
+
+}  // namespace milo
+
+using namespace milo;
+
+extern "C" int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H, int64_t F) {
+    if (!experts) return MILO_ERR_NULL;
+    if (E < 1 || E > 65536 || !w8_shape_ok(F, H) || !w8_shape_ok(H, F)) return MILO_ERR_SHAPE;
+    for (int e = 0; e < E; ++e) {
+        if (!experts[e].w1 || !experts[e].w3 || !experts[e].w2) return MILO_ERR_NULL;
+        if (!aligned16(experts[e].w1) || !aligned16(experts[e].w3) || !aligned16(experts[e].w2)) return MILO_ERR_ALIGN;
+    }
+    return MILO_OK;
+}
+
+extern "C" size_t milo_moe_w8a8_workspace(int64_t T, int64_t H, int64_t F, int E, int topk) {
+    W8MoeLayout L;
+    return w8_moe_layout(T, H, F, E, topk, &L) ? L.total : 0;
+}
+
+extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, int64_t F, const milo_w8_expert* experts, int E, const int32_t* topk_ids,
+                                     const float* topk_weights, int topk, unsigned flags, milo_half* Y, int32_t* status, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+    if (!X || !experts || !topk_ids || !topk_weights || !Y) return MILO_ERR_NULL;
+    W8MoeLayout L;
+    if ((flags & ~MILO_ACT_BF16) || !w8_moe_layout(T, H, F, E, topk, &L)) return MILO_ERR_SHAPE;
+    if (!workspace || workspace_bytes < L.total) return MILO_ERR_WORKSPACE;
+    if (!aligned16(X) || !aligned16(experts) || !aligned16(topk_ids) || !aligned16(topk_weights) || !aligned16(Y) || !aligned16(status) || !aligned16(workspace)) return MILO_ERR_ALIGN;
+    const bool bf = (flags & MILO_ACT_BF16) != 0;
+    const hipStream_t s = (hipStream_t)stream;
+    char* const ws = reinterpret_cast<char*>(workspace);
+    if (!status) status = reinterpret_cast<int32_t*>(ws + L.off_status);
+    const int64_t P = T * topk;
+    if (L.few) {
+        W8FewArgs a;
+        a.X = X;
+        a.T = (int)T;
+        a.topk = topk;
+        a.E = E;
+        a.H = H;
+        a.F = F;
+        a.experts = experts;
+        a.ids = topk_ids;
+        a.gates = topk_weights;
+        a.status = status;
+        a.h = reinterpret_cast<float*>(ws + L.off_h);
+        a.tops = reinterpret_cast<uint32_t*>(ws + L.off_tops);
+        a.Y = Y;
+        auto units = [&](int64_t K, int cap) {
+            const int64_t kb = w8_kblocks(K), most = cap / (64 * T);
+            return (int)(kb < most ? kb : most);
+        };
+        const int uu = units(H, kFewUpLds), ud = units(F, kFewDownLds);
+        const dim3 gu((unsigned)((F + 15) / 16), (unsigned)(P < E ? P : E)), gd((unsigned)((H + 15) / 16));
+        if (bf) w8_few_up_kernel<W8_BF16><<<gu, dim3(kFewUpThreads), uu * 64 * (int)T, s>>>(a, uu);
+        else w8_few_up_kernel<W8_F16><<<gu, dim3(kFewUpThreads), uu * 64 * (int)T, s>>>(a, uu);
+        int st = launch_status();
+        if (st != MILO_OK) return st;
+        if (bf) w8_few_down_kernel<true><<<gd, dim3(kFewDownThreads), ud * 64 * (int)T, s>>>(a, ud);
+        else w8_few_down_kernel<false><<<gd, dim3(kFewDownThreads), ud * 64 * (int)T, s>>>(a, ud);
+        return launch_status();
+    }
+    W8QuantArgs q;
+    q.in = X;
+    q.rows = T;
+    q.K = H;
+    q.codes = reinterpret_cast<uint8_t*>(ws + L.off_xq);
+    q.scales = reinterpret_cast<float*>(ws + L.off_xs);
+    q.blocked = 0;
+    int st = launch_w8_quant(q, bf ? W8_BF16 : W8_F16, s);
+    if (st != MILO_OK) return st;
+    RouteArgs g = {};
+    g.ids = topk_ids;
+    g.P = (int32_t)P;
+    g.E = E;
+    g.bm = L.bm;
+    g.topk = topk;
+    g.sorted = reinterpret_cast<int32_t*>(ws + L.off_sorted);
+    g.sorted_token = reinterpret_cast<int32_t*>(ws + L.off_token);
+    g.tiles = reinterpret_cast<TileDesc*>(ws + L.off_tiles);
+    g.header = status;
+    g.max_tiles = L.max_tiles;
+    st = launch_pair_groups(g, s);
+    if (st != MILO_OK) return st;
+    W8TileArgs t = {};
+    t.A = q.codes;
+    t.a_bytes = (uint64_t)(T * w8_kblocks(H) * 64);
+    t.a_scales = q.scales;
+    t.N = F;
+    t.K = H;
+    t.experts = experts;
+    t.tiles = g.tiles;
+    t.max_tiles = L.max_tiles;
+    t.x_rows = g.sorted_token;
+    t.out = ws + L.off_h;
+    st = launch_w8_tile(t, 1, L.bm, s);
+    if (st != MILO_OK) return st;
+    q.in = ws + L.off_h;
+    q.rows = P;
+    q.K = F;
+    q.codes = reinterpret_cast<uint8_t*>(ws + L.off_hq);
+    q.scales = reinterpret_cast<float*>(ws + L.off_hs);
+    st = launch_w8_quant(q, W8_F32, s);
+    if (st != MILO_OK) return st;
+    t.A = q.codes;
+    t.a_bytes = (uint64_t)(P * w8_kblocks(F) * 64);
+    t.a_scales = q.scales;
+    t.N = H;
+    t.K = F;
+    t.x_rows = g.sorted;
+    t.gates = topk_weights;
+    t.out = ws + L.off_o;
+    st = launch_w8_tile(t, 2, L.bm, s);
+    if (st != MILO_OK) return st;
+    const float* const O = reinterpret_cast<const float*>(ws + L.off_o);
+    if (bf) w8_combine_kernel<true><<<dim3((unsigned)T), dim3(256), 0, s>>>(O, topk_ids, topk, E, H, Y);
+    else w8_combine_kernel<false><<<dim3((unsigned)T), dim3(256), 0, s>>>(O, topk_ids, topk, E, H, Y);
+    return launch_status();
+}
