@@ -23,3 +23,4 @@ from .compensator import (svd_compensator, randomized_svd_compensator,  # noqa: 
 from .moe import moe_forward, silu                        # noqa: F401
 from .compress import (milo_compress, hqq_zero_points, shrink_lp, fixed_scales,  # noqa: F401
                        quantize_with, stop_rule)
+from .w8 import quantize_rows, w8a8_linear, moe_route, w8a8_moe   # noqa: F401

@@ -304,7 +304,8 @@ PyObject* py_w8_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const c10::DeviceGuard device(W->device());
         const int64_t N = W->size(0), K = W->size(1);
         const size_t bytes = e->w8_bytes(N, K);
-        at::Tensor blob = at::empty({(int64_t)(bytes > 16 ? bytes : 16)}, W->options().dtype(at::kByte));
+        if (bytes == 0) return status_object(MILO_ERR_SHAPE);
+        at::Tensor blob = at::empty({(int64_t)bytes}, W->options().dtype(at::kByte));
         const int st = e->w8_pack(W->data_ptr(), dt == at::kHalf ? MILO_F16 : dt == at::kBFloat16 ? MILO_BF16 : MILO_F32, N, K, blob.data_ptr(),
                                   current_stream());
         if (st != MILO_OK) return status_object(st);
@@ -325,6 +326,7 @@ PyObject* py_w8_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!blob || !whole(a[3], &N) || !whole(a[4], &K)) return nullptr;
         const int64_t M = X->size(0);
         if (X->size(1) != K) return PyErr_Format(PyExc_ValueError, "X and weight disagree on K");
+        if (M < 1) return status_object(MILO_ERR_SHAPE);        // (its tensors have no address)
         if ((size_t)blob->numel() < e->w8_bytes(N, K)) return PyErr_Format(PyExc_ValueError, "the packed weight is smaller than its shape says");
         const c10::DeviceGuard device(X->device());
         at::Tensor Y, ws;
@@ -351,7 +353,7 @@ PyObject* py_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (renormalize < 0) return nullptr;
         const int64_t T = X->size(0), H = X->size(1), E = Wg->size(0);
         if (Wg->size(1) != H) return PyErr_Format(PyExc_ValueError, "X and Wg disagree on H");
-        if (topk < 1 || topk > E || E > INT32_MAX || shared < 0 || shared > INT32_MAX) return status_object(MILO_ERR_SHAPE);
+        if (T < 1 || H < 1 || topk < 1 || topk > E || E > INT32_MAX || shared < 0 || shared > INT32_MAX) return status_object(MILO_ERR_SHAPE);
         const c10::DeviceGuard device(X->device());
         at::Tensor ids, gates;
         if (!output(a[6], at::kInt, T, topk + shared, *X, "ids", &ids) || !output(a[7], at::kFloat, T, topk + shared, *X, "gates", &gates)) return nullptr;
@@ -385,7 +387,7 @@ PyObject* py_w8_moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (X->size(1) != H) return PyErr_Format(PyExc_ValueError, "X must have H columns");
         if (ids->size(0) != T || gates->size(0) != T || gates->size(1) != topk)
             return PyErr_Format(PyExc_ValueError, "ids and gates must have the same shape, with a row for every row of X");
-        if (topk > INT32_MAX || E > INT32_MAX || (size_t)table->numel() < (size_t)E * sizeof(milo_w8_expert)) return status_object(MILO_ERR_SHAPE);
+        if (T < 1 || topk < 1 || topk > INT32_MAX || E > INT32_MAX || (size_t)table->numel() < (size_t)E * sizeof(milo_w8_expert)) return status_object(MILO_ERR_SHAPE);
         const c10::DeviceGuard device(X->device());
         at::Tensor Y, ws;
         if (!output(a[8], X->scalar_type(), T, H, *X, "out", &Y) || !scratch(a[10], e->w8_moe_workspace(T, H, F, (int)E, (int)topk), *X, &ws)) return nullptr;
