@@ -34,7 +34,7 @@ struct W8TileArgs {
     const void* w;                  // EPI 0
     const milo_w8_expert* experts;  // EPI 1, 2: device table
     const TileDesc* tiles;
-    int max_tiles;
+    int m_tiles, n_tiles;           // EPI 1, 2: m_tiles slots, some of them empty; the rest is set by launch_w8_tile
     const int32_t* x_rows;          // EPI 1: token of a sorted row;  EPI 2: pair of a sorted row
     const float* gates;             // EPI 2: factor per pair
     void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N] fp32

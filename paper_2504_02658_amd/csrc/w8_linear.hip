@@ -1,4 +1,6 @@
 // Linears in 8-bit integers: milo_pack_w8, milo_w8a8_gemm and the tiled product that the MoE layer shares.
+#include <type_traits>
+
 #include "milo_host.h"
 #include "w8_kernels.h"
 
@@ -114,28 +116,44 @@ __global__ __launch_bounds__(kStreamWaves * 64) void w8_stream_kernel(const uint
 }
 
 // ---------------------------------------------------------------------------------------------
+// Tile of a workgroup.  Workgroup i runs on XCD i % 8, each of which has an L2 of its own, so every XCD gets a contiguous range of
+// an order in which tiles that share rows or columns are close: groups of kGroupM tiles of rows, and inside a group all columns,
+// rows fastest.
+constexpr int kGroupM = 8;
+__device__ __forceinline__ void tile_of(uint32_t i, int m_tiles, int n_tiles, int* mt, int* nt) {
+    const uint32_t total = (uint32_t)m_tiles * (uint32_t)n_tiles, x = i & 7u, per = total >> 3, rem = total & 7u;
+    const uint32_t l = x * per + (x < rem ? x : rem) + (i >> 3);
+    const uint32_t group = l / (uint32_t)(kGroupM * n_tiles), in = l - group * (uint32_t)(kGroupM * n_tiles);
+    const uint32_t left = (uint32_t)m_tiles - group * kGroupM, rows = left < kGroupM ? left : kGroupM;
+    *nt = (int)(in / rows);
+    *mt = (int)(group * kGroupM + in % rows);
+}
+
 // The tiled product.
-template <int WM, int WN, int TM, int TN, int EPI, bool BF>
+template <int WM, int WN, int TM, int TN, int NS, int EPI, bool BF>
 __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs a) {
     constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
-    constexpr int ABLK = BM / 8, BBLK = BN / 8, BLK = ABLK + BBLK, PER = BLK / NW;     // 1-KB blocks of a stage (128 columns)
-    constexpr int STAGE = BLK * 1024;
+    constexpr int ABLK = BM / 16, BBLK = BN / 16;       // 1-KB blocks of a stage (64 columns)
+    constexpr int PA = ABLK / NW, PB = BBLK / NW;       // of them, copied by one wave
+    constexpr int STAGE = (ABLK + BBLK) * 1024;
     constexpr int OUTN = EPI == 1 ? BN / 2 : BN;        // output columns of a tile
-    static_assert(BLK % NW == 0, "every wave copies as many blocks");
+    static_assert(ABLK % NW == 0 && (EPI == 1 ? BBLK / 2 : BBLK) % NW == 0, "every wave copies as many blocks");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kb = (int)w8_kblocks(a.K), chunks = kb / 2;
-    const int64_t n0 = (int64_t)blockIdx.x * OUTN;
+    const int kb = (int)w8_kblocks(a.K);
+    int mt, nt;
+    tile_of(blockIdx.x, a.m_tiles, a.n_tiles, &mt, &nt);
+    const int64_t n0 = (int64_t)nt * OUTN;
     int64_t row0;
     int rows;
     const uint8_t* w0;
     const uint8_t* w1;
     if constexpr (EPI == 0) {
-        row0 = (int64_t)blockIdx.y * BM;
+        row0 = (int64_t)mt * BM;
         rows = (int)(a.M - row0 < BM ? a.M - row0 : BM);
         w0 = w1 = reinterpret_cast<const uint8_t*>(a.w);
     } else {
-        const TileDesc t = a.tiles[blockIdx.y];
+        const TileDesc t = a.tiles[mt];
         row0 = t.row0;
         rows = t.rows;
         if (rows == 0) return;
@@ -143,41 +161,44 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
         w0 = reinterpret_cast<const uint8_t*>(EPI == 1 ? e.w1 : e.w2);
         w1 = reinterpret_cast<const uint8_t*>(EPI == 1 ? e.w3 : e.w2);
     }
-    // where this wave's copies come from: activations first, then the weight (gate and up: half of the rows each)
+    // where this wave's copies come from: activations, then the weight (gate and up: half of the rows each)
     const uint64_t wbytes = (uint64_t)w8_code_bytes(a.N, a.K), wskip = (uint64_t)(n0 >> 4) * kb * 1024;
     const uint64_t abase = EPI == 0 ? (uint64_t)row0 / 16 * kb * 1024 : 0;
     const BufRsrc ra = make_rsrc(a.A + abase, a.a_bytes - abase);
     const BufRsrc rb0 = make_rsrc(w0 + wskip, wbytes - wskip), rb1 = make_rsrc(w1 + wskip, wbytes - wskip);
-    uint32_t off[PER];
+    uint32_t aoff[PA], boff[PB];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
+    for (int i = 0; i < PA; ++i) {
         const int b = wave + i * NW;
-        if (b < ABLK) {
-            if constexpr (EPI == 0) {
-                off[i] = (uint32_t)((b >> 1) * kb + (b & 1)) * 1024u + lane * 16;
-            } else {
-                int r = (b >> 1) * 16 + (lane & 15);
-                r = (int)row0 + (r < rows ? r : 0);         // (rows beyond the tile's: computed, not stored)
-                const int64_t src = EPI == 1 ? a.x_rows[r] : r;
-                off[i] = (uint32_t)(src * kb * 64) + (b & 1) * 64 + (lane >> 4) * 16;
-            }
+        if constexpr (EPI == 0) {
+            aoff[i] = (uint32_t)(b * kb) * 1024u + lane * 16;
         } else {
-            const int j = b - ABLK, n16 = (j >> 1) % (OUTN / 16);
-            off[i] = (uint32_t)(n16 * kb + (j & 1)) * 1024u + lane * 16;
+            int r = b * 16 + (lane & 15);
+            r = (int)row0 + (r < rows ? r : 0);         // (rows beyond the tile's: computed, not stored)
+            const int64_t src = EPI == 1 ? a.x_rows[r] : r;
+            aoff[i] = (uint32_t)(src * kb * 64) + (lane >> 4) * 16;
         }
     }
-    auto issue = [&](int c, int stage) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int b = wave + i * NW;
-            const uint32_t o = off[i] + (uint32_t)c * (b < ABLK && EPI != 0 ? 128u : 2048u);
-            const BufRsrc r = b < ABLK ? ra : (b - ABLK) < 2 * (OUTN / 16) ? rb0 : rb1;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsDst)(smem + stage * STAGE + b * 1024), 16, o, 0, 0, 0);
+    for (int i = 0; i < PB; ++i) boff[i] = (uint32_t)(((wave + i * NW) % (OUTN / 16)) * kb) * 1024u + lane * 16;
+    auto issue = [&](int c) {
+        unsigned char* const to = smem + (c % NS) * STAGE + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const uint32_t o = aoff[i];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsDst)(to + i * NW * 1024), 16, o, 0, 0, 0);
+            aoff[i] += EPI == 0 ? 1024u : 64u;
         }
-        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const uint32_t o = boff[i];
+            if (EPI == 1 && i >= PB / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rb1, (LdsDst)(to + (ABLK + i * NW) * 1024), 16, o, 0, 0, 0);
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(rb0, (LdsDst)(to + (ABLK + i * NW) * 1024), 16, o, 0, 0, 0);
+            boff[i] += 1024u;
+        }
     };
     const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, h = lane >> 5;
-    const int frag = (l32 >> 4) * 2048 + h * 256 + (l32 & 15) * 16;
+    const int frag = (l32 >> 4) * 1024 + h * 256 + (l32 & 15) * 16;
     i32x16 acc[TN][TM];
 #pragma unroll
     for (int n = 0; n < TN; ++n)
@@ -187,32 +208,59 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
             for (int i = 0; i < 16; ++i) acc[n][m][i] = 0;
     // rows (of 32) of the weight's part of a stage that the wave's n-th tile reads
     auto brow = [&](int n) { return EPI == 1 ? (n < TN / 2 ? wn * (TN / 2) + n : OUTN / 32 + wn * (TN / 2) + n - TN / 2) : wn * TN + n; };
-    issue(0, 0);
-    for (int c = 0; c < chunks; ++c) {
-        if (c + 1 < chunks) {
-            issue(c + 1, (c + 1) & 1);
-            MILO_WAIT_VMEM(PER);
-        } else {
-            MILO_WAIT_VMEM(0);
+    // A stage is 64 columns, two steps of 32.  While the matrix cores work on one step the fragments of the next one are on their
+    // way from LDS.  The copies of a wave complete in order: with at most those of the NS - 2 younger stages outstanding, stage
+    // c + 1 is there; the barrier says so for all waves, and that all have read what they need of stage c, whose place the next
+    // copies take.
+    u32x4 af[2][TM], bf[2][TN];
+    auto read = [&](int c, int k) {
+        const unsigned char* const as = smem + (c % NS) * STAGE + wm * TM * 2048 + frag + k * 512;
+        const unsigned char* const bs = smem + (c % NS) * STAGE + ABLK * 1024 + frag + k * 512;
+#pragma unroll
+        for (int n = 0; n < TN; ++n) bf[k][n] = *reinterpret_cast<const u32x4*>(bs + brow(n) * 2048);
+#pragma unroll
+        for (int m = 0; m < TM; ++m) af[k][m] = *reinterpret_cast<const u32x4*>(as + m * 2048);
+    };
+    auto multiply = [&](int k) {
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int n = 0; n < TN; ++n) acc[n][m] = mfma32_i8(bf[k][n], af[k][m], acc[n][m]);
+    };
+    // one LDS read behind each of the first matrix instructions, instead of all of them in front
+    auto mix = [&] {
+#pragma unroll
+        for (int i = 0; i < TM + TN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
         }
-        __syncthreads();
-        const unsigned char* as = smem + (c & 1) * STAGE + wm * TM * 4096 + frag;
-        const unsigned char* bs = smem + (c & 1) * STAGE + ABLK * 1024 + frag;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int ko = (k >> 1) * 1024 + (k & 1) * 512;
-            u32x4 af[TM], bf[TN];
-#pragma unroll
-            for (int m = 0; m < TM; ++m) af[m] = *reinterpret_cast<const u32x4*>(as + m * 4096 + ko);
-#pragma unroll
-            for (int n = 0; n < TN; ++n) bf[n] = *reinterpret_cast<const u32x4*>(bs + brow(n) * 4096 + ko);
-#pragma unroll
-            for (int n = 0; n < TN; ++n)
-#pragma unroll
-                for (int m = 0; m < TM; ++m) acc[n][m] = mfma32_i8(bf[n], af[m], acc[n][m]);
-        }
-        __syncthreads();
-    }
+        __builtin_amdgcn_sched_group_barrier(0x8, TM * TN - TM - TN, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto arrive = [&](auto counted, bool all) {
+        if (!decltype(counted)::value && all) wait_vmem();
+        else MILO_WAIT_VMEM((NS - 2) * (PA + PB));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    for (int c = 0; c < NS - 1 && c < kb; ++c) issue(c);
+    arrive(std::bool_constant<false>{}, kb < NS - 1);
+    if (NS - 1 < kb) issue(NS - 1);
+    read(0, 0);
+    int c = 0;
+    auto stage = [&](auto more) {           // more: stage c + NS exists
+        read(c, 1);
+        multiply(0);
+        mix();
+        arrive(more, true);
+        if constexpr (decltype(more)::value) issue(c + NS);
+        read(c + 1, 0);                     // (behind the last stage: of no use)
+        multiply(1);
+        mix();
+    };
+    for (; c + NS < kb; ++c) stage(std::bool_constant<true>{});
+    for (; c < kb; ++c) stage(std::bool_constant<false>{});
     // lane: row (of 32) l32, output features 8 i + 4 h + 0..3
     const bool vec = (a.N & 3) == 0;
     const float* const sw0 = w8_scales(w0, a.N, a.K);
@@ -255,30 +303,33 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
     }
 }
 
-template <int WM, int WN, int TM, int TN, int EPI, bool BF>
-static int launch_tile(const W8TileArgs& a, hipStream_t stream) {
-    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, OUTN = EPI == 1 ? BN / 2 : BN, lds = 2 * (BM + BN) * 128;
+template <int WM, int WN, int TM, int TN, int NS, int EPI, bool BF>
+static int launch_tile(W8TileArgs a, hipStream_t stream) {
+    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, OUTN = EPI == 1 ? BN / 2 : BN, lds = NS * (BM + BN) * 64;
     if constexpr (lds > 64 * 1024) {
         static bool raised[64] = {false};
         int dev = 0;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MILO_ERR_HIP;
         if (!raised[dev]) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_tile_kernel<WM, WN, TM, TN, EPI, BF>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_tile_kernel<WM, WN, TM, TN, NS, EPI, BF>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
                 return MILO_ERR_HIP;
             raised[dev] = true;
         }
     }
-    const int64_t gy = EPI == 0 ? (a.M + BM - 1) / BM : a.max_tiles;
-    w8_tile_kernel<WM, WN, TM, TN, EPI, BF><<<dim3((unsigned)((a.N + OUTN - 1) / OUTN), (unsigned)gy), dim3(WM * WN * 64), lds, stream>>>(a);
+    if (EPI == 0) a.m_tiles = (int)((a.M + BM - 1) / BM);
+    a.n_tiles = (int)((a.N + OUTN - 1) / OUTN);
+    if ((int64_t)a.m_tiles * a.n_tiles > (int64_t(1) << 31) / (WM * WN * 64)) return MILO_ERR_SHAPE;
+    w8_tile_kernel<WM, WN, TM, TN, NS, EPI, BF><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(WM * WN * 64), lds, stream>>>(a);
     return launch_status();
 }
+template <int EPI, bool BF>
+static int launch_tile_bm(const W8TileArgs& a, int bm, hipStream_t stream) {
+    if (bm == 256) return launch_tile<2, 4, 4, 2, 4, EPI, BF>(a, stream);
+    return launch_tile<2, 2, 2, 2, 4, EPI, BF>(a, stream);
+}
 int launch_w8_tile(const W8TileArgs& a, int epi, int bm, hipStream_t stream) {
-    if (epi == 0) {
-        if (bm == 256) return a.act_bf16 ? launch_tile<2, 4, 4, 2, 0, true>(a, stream) : launch_tile<2, 4, 4, 2, 0, false>(a, stream);
-        return a.act_bf16 ? launch_tile<2, 2, 2, 2, 0, true>(a, stream) : launch_tile<2, 2, 2, 2, 0, false>(a, stream);
-    }
-    if (epi == 1) return bm == 256 ? launch_tile<2, 4, 4, 2, 1, false>(a, stream) : launch_tile<2, 2, 2, 2, 1, false>(a, stream);
-    return bm == 256 ? launch_tile<2, 4, 4, 2, 2, false>(a, stream) : launch_tile<2, 2, 2, 2, 2, false>(a, stream);
+    if (epi == 0) return a.act_bf16 ? launch_tile_bm<0, true>(a, bm, stream) : launch_tile_bm<0, false>(a, bm, stream);
+    return epi == 1 ? launch_tile_bm<1, false>(a, bm, stream) : launch_tile_bm<2, false>(a, bm, stream);
 }
 
 }  // namespace milo

@@ -377,7 +377,7 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.K = H;
     t.experts = experts;
     t.tiles = g.tiles;
-    t.max_tiles = L.max_tiles;
+    t.m_tiles = L.max_tiles;
     t.x_rows = g.sorted_token;
     t.out = ws + L.off_h;
     st = launch_w8_tile(t, 1, L.bm, s);
