@@ -440,7 +440,7 @@ int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H,
  * Top-k routed MoE feed-forward layer over W8A8 experts:
  *     y_t = sum_j gates[t,j] * lin_w2^e( SiLU(lin_w1^e(x_t)) * lin_w3^e(x_t) ),   e = ids[t,j]
  * with every lin the W8A8 linear above: a token's activations are quantized once, the SwiGLU output of a (token, expert) pair is
- * a row of its own, and it is quantized from fp32.  Up to 16 tokens (256 pairs) two launches, reading the weights of the experts
+ * a row of its own, and it is quantized from fp32.  Up to 16 tokens (128 pairs) two launches, reading the weights of the experts
  * that occur; more tokens are grouped per expert inside the call.
  *   X  [T x H] fp16, or bfloat16 with MILO_ACT_BF16;  Y the same
  *   experts      DEVICE array of E entries (a byte copy of a table that passed milo_moe_w8a8_check_experts)

@@ -56,11 +56,43 @@ __device__ __forceinline__ int row_code(float x, const RowStep& r) {
 __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
     return (uint32_t)(a & 255) | (uint32_t)(b & 255) << 8 | (uint32_t)(c & 255) << 16 | (uint32_t)d << 24;
 }
+// The low bytes of four words.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+    return lo | hi;
+}
+constexpr float kRoundMagic = 12582912.0f;      // 1.5 * 2^23: a sum with it has the nearest whole number in its low bits, half to even
+// 16 codes.  The rounding of the product is the code unless the remainder is half a step or more, which a tie or
+// a quotient within 2^-17 of one does: only then the elements go one by one.
 __device__ __forceinline__ u32x4 row_codes16(const float (&v)[16], const RowStep& r) {
+    uint32_t b[16];
+    float far = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float t = fmaf(v[i], r.inv, kRoundMagic);
+        b[i] = __float_as_uint(t);
+        far = fmaxf(far, fabsf(fmaf(-(t - kRoundMagic), r.s, v[i])));
+    }
     u32x4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        o[i] = pack4(row_code(v[4 * i], r), row_code(v[4 * i + 1], r), row_code(v[4 * i + 2], r), row_code(v[4 * i + 3], r));
+    for (int i = 0; i < 4; ++i) o[i] = low_bytes(b[4 * i], b[4 * i + 1], b[4 * i + 2], b[4 * i + 3]);
+    if (far >= r.half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] = pack4(row_code(v[4 * i], r), row_code(v[4 * i + 1], r), row_code(v[4 * i + 2], r), row_code(v[4 * i + 3], r));
+    }
+    return o;
+}
+// The same for values that carry a rounding of their own (the SwiGLU output): the product's rounding is as good as any.
+__device__ __forceinline__ u32x4 near_codes16(const float (&v)[16], float inv) {
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(fmaf(v[4 * i + j], inv, kRoundMagic));
+        o[i] = low_bytes(b[0], b[1], b[2], b[3]);
+    }
     return o;
 }
 
@@ -70,11 +102,22 @@ template <int IN> struct W8Raw { uint32_t w[IN == W8_F32 ? 16 : 8]; };      // 1
 
 // Elements [k, k + 16) of a row of K, zeros beyond it.  The row may start at any element's address: whole pieces are
 // copied by the widest loads (which need no alignment here), the last one element by element.
-template <int IN>
+// WHOLE: the piece is known to lie inside, and the row to start at a 16-byte boundary.
+template <int IN, bool WHOLE = false>
 __device__ __forceinline__ W8Raw<IN> load16(const void* row, int64_t k, int64_t K) {
     constexpr int SZ = IN == W8_F32 ? 4 : 2;
     W8Raw<IN> r;
     const char* p = reinterpret_cast<const char*>(row) + k * SZ;
+    if constexpr (WHOLE) {
+        const u32x4* const q = reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < SZ; ++i) {
+            const u32x4 v = q[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.w[4 * i + j] = v[j];
+        }
+        return r;
+    }
     if (k + 16 <= K) {
         __builtin_memcpy(&r, p, 16 * SZ);
     } else {

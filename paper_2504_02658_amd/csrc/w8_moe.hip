@@ -13,9 +13,8 @@
 
 namespace milo {
 
-constexpr int kFewTokens = 16, kFewMaxPairs = 256;
+constexpr int kFewTokens = 16, kFewMaxPairs = 128;
 constexpr int kFewUpThreads = 256, kFewDownThreads = 512;
-constexpr int kFewUpLds = 48 * 1024, kFewDownLds = 48 * 1024;       // most bytes of codes that a workgroup holds at once
 
 struct W8FewArgs {
     const void* X;
@@ -31,7 +30,7 @@ struct W8FewArgs {
 };
 
 // The experts that occur in the ids, in the order of their first occurrence: their number, and in list[i] the i-th
-// one's id for all i below it.  All threads of the workgroup take part; s_ids receives the ids, -1 for one out of range.
+// one's id.  All threads of the workgroup take part; s_ids receives the ids, -1 for one out of range.
 template <int THREADS>
 __device__ __forceinline__ int distinct_experts(const W8FewArgs& a, int32_t* s_ids, int32_t* s_list, int32_t* s_count, bool* bad) {
     static_assert(THREADS >= kFewMaxPairs, "a thread per pair");
@@ -44,13 +43,17 @@ __device__ __forceinline__ int distinct_experts(const W8FewArgs& a, int32_t* s_i
     if (tid < kFewMaxPairs) s_ids[tid] = id;
     *bad = __syncthreads_or(tid < P && id < 0) != 0;
     bool first = id >= 0;
-    for (int q = 0; q < P; ++q) first = first && !(q < tid && s_ids[q] == id);
+    if (tid < kFewMaxPairs)
+        for (int q = 0; q < P; q += 4) {
+            const int4 v = *reinterpret_cast<const int4*>(s_ids + q);       // (entries from P on are -1)
+            first = first && !(v.x == id && q < tid) && !(v.y == id && q + 1 < tid) && !(v.z == id && q + 2 < tid) && !(v.w == id && q + 3 < tid);
+        }
     const unsigned long long m = __builtin_amdgcn_ballot_w64(first);
     if ((tid & 63) == 0) s_count[tid >> 6] = __popcll(m);
     __syncthreads();
     int at = __popcll(m & ((1ull << (tid & 63)) - 1ull)), total = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
+    for (int w = 0; w < kFewMaxPairs / 64; ++w) {
         at += w < (tid >> 6) ? s_count[w] : 0;
         total += s_count[w];
     }
@@ -65,15 +68,19 @@ __device__ __forceinline__ int slot_of(const int32_t* s_ids, int topk, int t, in
     return found;
 }
 
-// Codes in LDS: 64-column unit u of token t, piece c of 16 columns, at ((u * 4 + c) * T + t) * 16.
-template <int IN>
-__global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArgs a, int lds_units) {
-    constexpr int NW = kFewUpThreads / 64;
-    __shared__ int32_t s_ids[kFewMaxPairs], s_list[kFewMaxPairs], s_count[NW];
+// Both kernels: column m of an operand of the matrix cores is token m, and lane (m, c) quantizes the 16 values of token m that it
+// holds of it itself, from the row's scale, straight from memory (the rows are small and stay in the caches); a
+// wave works on kFewBatch fragments of the weight at a time, and has the next ones on their way.
+constexpr int kFewBatch = 4;
+
+template <int IN, bool WHOLE>
+__global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArgs a) {
+    constexpr int NW = kFewUpThreads / 64, B = kFewBatch;
+    __shared__ __attribute__((aligned(16))) int32_t s_ids[kFewMaxPairs];
+    __shared__ int32_t s_list[kFewMaxPairs], s_count[NW];
     __shared__ int32_t s_slot[kFewTokens];
     __shared__ RowStep s_step[kFewTokens];
     __shared__ i32x4 s_part[2][NW][64];
-    extern __shared__ __attribute__((aligned(16))) unsigned char codes[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int slot = blockIdx.y;
     bool bad;
@@ -81,42 +88,64 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     if (blockIdx.x == 0 && slot == 0 && tid == 0) a.status[0] = bad ? MILO_ERR_ROUTING : MILO_OK;
     if (slot >= total) return;
     const int e = __builtin_amdgcn_readfirstlane(s_list[slot]);
+    const int kb = (int)w8_kblocks(a.H);
+    const void* const p1 = a.experts[e].w1;
+    const void* const p3 = a.experts[e].w3;
+    const int64_t wskip = (int64_t)blockIdx.x * kb * 1024;
+    const u32x4* const w1 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p1) + wskip) + lane;
+    const u32x4* const w3 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p3) + wskip) + lane;
+    u32x4 f1[2][B], f3[2][B];
+    auto fetch = [&](int u, int to) {               // fragments u, u + NW, .. (past the end: the last one, for nothing)
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            const int v = u + i * NW < kb ? u + i * NW : kb - 1;
+            f1[to][i] = w1[(int64_t)v * 64];
+            f3[to][i] = w3[(int64_t)v * 64];
+        }
+    };
+    fetch(wave, 0);
     if (tid < kFewTokens) s_slot[tid] = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
     __syncthreads();
     const char* const X = reinterpret_cast<const char*>(a.X);
-    const int kb = (int)w8_kblocks(a.H);
     for (int t = wave; t < a.T; t += NW) {
         if (s_slot[t] < 0) continue;
         uint32_t top = 0u;
-        for (int p = lane; p < kb * 4; p += 64) top = raw_top<IN>(load16<IN>(X + t * a.H * 2, (int64_t)p * 16, a.H), top);
+        for (int p = lane; p < (int)((a.H + 15) / 16); p += 64) top = raw_top<IN>(load16<IN, WHOLE>(X + t * a.H * 2, (int64_t)p * 16, a.H), top);
         top = wave_max(top);
         if (lane == 0) s_step[t] = row_step(top);
     }
-    const milo_w8_expert& ex = a.experts[e];
-    const int64_t wskip = (int64_t)blockIdx.x * kb * 1024;
-    const u32x4* const w1 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(ex.w1) + wskip) + lane;
-    const u32x4* const w3 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(ex.w3) + wskip) + lane;
-    i32x4 acc1 = {0, 0, 0, 0}, acc3 = {0, 0, 0, 0};
+    __syncthreads();
     const int m = lane & 15, c16 = lane >> 4;
     const bool mine = m < a.T && s_slot[m] >= 0;
-    for (int u0 = 0; u0 < kb; u0 += lds_units) {
-        const int units = kb - u0 < lds_units ? kb - u0 : lds_units;
-        __syncthreads();
-        for (int i = tid; i < units * 4 * a.T; i += kFewUpThreads) {
-            const int t = i % a.T, p = i / a.T;
-            if (s_slot[t] < 0) continue;
-            float v[16];
-            raw_values<IN>(load16<IN>(X + t * a.H * 2, (int64_t)(u0 * 4 + p) * 16, a.H), v);
-            *reinterpret_cast<u32x4*>(codes + i * 16) = row_codes16(v, s_step[t]);
+    const RowStep step = s_step[m];
+    const char* const x = X + (mine ? m : 0) * a.H * 2;
+    i32x4 acc1 = {0, 0, 0, 0}, acc3 = {0, 0, 0, 0};
+    auto work = [&](int u, int from) {
+        W8Raw<IN> raw[B];
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+                if (u + i * NW < kb) raw[i] = load16<IN, WHOLE>(x, (int64_t)(u + i * NW) * 64 + c16 * 16, a.H);
         }
-        __syncthreads();
-#pragma unroll 4
-        for (int u = wave; u < units; u += NW) {
-            u32x4 x = {0u, 0u, 0u, 0u};
-            if (mine) x = *reinterpret_cast<const u32x4*>(codes + ((u * 4 + c16) * a.T + m) * 16);
-            acc1 = mfma16_i8(w1[(int64_t)(u0 + u) * 64], x, acc1);
-            acc3 = mfma16_i8(w3[(int64_t)(u0 + u) * 64], x, acc3);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (u + i * NW >= kb) break;
+            u32x4 q = {0u, 0u, 0u, 0u};
+            if (mine) {
+                float v[16];
+                raw_values<IN>(raw[i], v);
+                q = row_codes16(v, step);
+            }
+            acc1 = mfma16_i8(f1[from][i], q, acc1);
+            acc3 = mfma16_i8(f3[from][i], q, acc3);
         }
+    };
+    for (int u = wave; u < kb; u += 2 * B * NW) {
+        fetch(u + B * NW, 1);
+        work(u, 0);
+        if (u + B * NW >= kb) break;
+        fetch(u + 2 * B * NW, 0);
+        work(u + B * NW, 1);
     }
     s_part[0][wave][lane] = acc1;
     s_part[1][wave][lane] = acc3;
@@ -131,13 +160,12 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     uint32_t top = 0u;
     const int64_t row = mine ? m * a.topk + s_slot[m] : 0;
     if (mine) {
-        const float* const sw1 = w8_scales(ex.w1, a.F, a.H) + n;
-        const float* const sw3 = w8_scales(ex.w3, a.F, a.H) + n;
-        const float sx = s_step[m].s;
+        const float* const sw1 = w8_scales(p1, a.F, a.H) + n;
+        const float* const sw3 = w8_scales(p3, a.F, a.H) + n;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (n + i >= a.F) continue;
-            const float v = silu_times((float)acc1[i] * sx * sw1[i], (float)acc3[i] * sx * sw3[i]);
+            const float v = silu_times((float)acc1[i] * step.s * sw1[i], (float)acc3[i] * step.s * sw3[i]);
             a.h[row * a.F + n + i] = v;
             const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
             top = b > top ? b : top;
@@ -151,78 +179,127 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     if (mine && c16 == 0) a.tops[row * ((a.F + 15) / 16) + blockIdx.x] = top;
 }
 
-template <bool BF>
-__global__ __launch_bounds__(kFewDownThreads) void w8_few_down_kernel(const W8FewArgs a, int lds_units) {
-    constexpr int NW = kFewDownThreads / 64;
-    __shared__ int32_t s_ids[kFewMaxPairs], s_list[kFewMaxPairs], s_count[NW];
-    __shared__ int32_t s_slot[kFewTokens];
-    __shared__ RowStep s_step[kFewTokens];
-    __shared__ float s_gate[kFewTokens];
+// The fragments of all experts' weights are one sequence, which the waves share; a wave adds up an expert's products
+// in integers and turns to fp32 where it goes on to the next expert.
+template <bool BF, bool WHOLE>
+__global__ __launch_bounds__(kFewDownThreads) void w8_few_down_kernel(const W8FewArgs a) {
+    constexpr int NW = kFewDownThreads / 64, B = kFewBatch;
+    __shared__ __attribute__((aligned(16))) int32_t s_ids[kFewMaxPairs];
+    __shared__ int32_t s_list[kFewMaxPairs], s_count[NW];
+    __shared__ RowStep s_step[kFewMaxPairs];                        // per pair
+    __shared__ const void* s_w[kFewMaxPairs];                       // per expert that occurs: its weight,
+    __shared__ float s_sw[kFewMaxPairs][16];                        // the scales of this workgroup's features,
+    __shared__ int16_t s_row[kFewMaxPairs][kFewTokens];             // the tokens' rows of H (-1: none)
+    __shared__ float s_gate[kFewMaxPairs][kFewTokens];              // and their weights
     __shared__ f32x4 s_part[NW][64];
-    extern __shared__ __attribute__((aligned(16))) unsigned char codes[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kb = (int)w8_kblocks(a.F), nt = (int)((a.F + 15) / 16), P = a.T * a.topk;
     bool bad;
     const int total = distinct_experts<kFewDownThreads>(a, s_ids, s_list, s_count, &bad);
-    const int kb = (int)w8_kblocks(a.F), nt = (int)((a.F + 15) / 16);
-    const int m = lane & 15, c16 = lane >> 4;
-    const int64_t n = (int64_t)blockIdx.x * 16 + c16 * 4;
-    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < total; ++s) {
-        const int e = __builtin_amdgcn_readfirstlane(s_list[s]);
-        __syncthreads();
-        if (tid < kFewTokens) {
-            const int j = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
-            s_slot[tid] = j;
-            float g = 0.0f;
-            if (j >= 0)
-                for (int i = 0; i < a.topk; ++i) g += s_ids[tid * a.topk + i] == e ? a.gates[tid * a.topk + i] : 0.0f;
-            s_gate[tid] = g;
-        }
-        __syncthreads();
-        for (int t = wave; t < a.T; t += NW) {
-            if (s_slot[t] < 0) continue;
-            uint32_t top = 0u;
-            const uint32_t* const tops = a.tops + (int64_t)(t * a.topk + s_slot[t]) * nt;
-            for (int i = lane; i < nt; i += 64) top = tops[i] > top ? tops[i] : top;
-            top = wave_max(top);
-            if (lane == 0) s_step[t] = row_step(top);
-        }
-        const void* const w2 = a.experts[e].w2;
-        const u32x4* const w = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(w2) + (int64_t)blockIdx.x * kb * 1024) + lane;
-        i32x4 acc = {0, 0, 0, 0};
-        const bool mine = m < a.T && s_slot[m] >= 0;
-        for (int u0 = 0; u0 < kb; u0 += lds_units) {
-            const int units = kb - u0 < lds_units ? kb - u0 : lds_units;
-            __syncthreads();
-            for (int i = tid; i < units * 4 * a.T; i += kFewDownThreads) {
-                const int t = i % a.T, p = i / a.T;
-                if (s_slot[t] < 0) continue;
-                float v[16];
-                raw_values<W8_F32>(load16<W8_F32>(a.h + (int64_t)(t * a.topk + s_slot[t]) * a.F, (int64_t)(u0 * 4 + p) * 16, a.F), v);
-                *reinterpret_cast<u32x4*>(codes + i * 16) = row_codes16(v, s_step[t]);
-            }
-            __syncthreads();
-#pragma unroll 4
-            for (int u = wave; u < units; u += NW) {
-                u32x4 x = {0u, 0u, 0u, 0u};
-                if (mine) x = *reinterpret_cast<const u32x4*>(codes + ((u * 4 + c16) * a.T + m) * 16);
-                acc = mfma16_i8(w[(int64_t)(u0 + u) * 64], x, acc);
-            }
-        }
-        if (mine && n < a.H) {
-            const float* const sw = w8_scales(w2, a.H, a.F) + n;        // (there are scales for whole blocks of 16)
-            const float f = s_step[m].s;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * f * sw[i] * s_gate[m];
-        }
+    for (int p = wave; p < P; p += NW) {
+        if (s_ids[p] < 0) continue;
+        uint32_t top = 0u;
+        const uint32_t* const tops = a.tops + (int64_t)p * nt;
+        for (int i = lane; i < nt; i += 64) top = tops[i] > top ? tops[i] : top;
+        top = wave_max(top);
+        if (lane == 0) s_step[p] = row_step(top);
     }
+    for (int i = tid; i < total * 16; i += kFewDownThreads) {
+        const int s = i >> 4, m = i & 15, e = s_list[s];
+        const void* const w = a.experts[e].w2;
+        if (m == 0) s_w[s] = w;
+        s_sw[s][m] = w8_scales(w, a.H, a.F)[(int64_t)blockIdx.x * 16 + m];
+        const int j = m < a.T ? slot_of(s_ids, a.topk, m, e) : -1;
+        float g = 0.0f;
+        if (j >= 0)
+            for (int k = 0; k < a.topk; ++k) g += s_ids[m * a.topk + k] == e ? a.gates[m * a.topk + k] : 0.0f;
+        s_row[s][m] = (int16_t)(j >= 0 ? m * a.topk + j : -1);
+        s_gate[s][m] = g;
+    }
+    __syncthreads();
+    const int m = lane & 15, c16 = lane >> 4, units = total * kb;
+    const int64_t skip = (int64_t)blockIdx.x * kb * 64 + lane;
+    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    i32x4 acc = {0, 0, 0, 0};
+    // unit g: fragment g % kb of expert g / kb.  One batch of units: of which expert and fragment, its weight and its rows of H
+    int slot[2][B];
+    u32x4 w[2][B];
+    W8Raw<W8_F32> raw[2][B];
+    int fs = 0, fu = wave;                          // the next unit to fetch
+    auto fetch = [&](int to) {
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            while (fu >= kb) {
+                fu -= kb;
+                ++fs;
+            }
+            slot[to][i] = fs;
+            if (fs < total) {
+                w[to][i] = (reinterpret_cast<const u32x4*>(s_w[fs]) + skip)[(int64_t)fu * 64];
+                const int row = s_row[fs][m];
+                if (row >= 0) raw[to][i] = load16<W8_F32, WHOLE>(a.h + (int64_t)row * a.F, (int64_t)fu * 64 + c16 * 16, a.F);
+            }
+            fu += NW;
+        }
+    };
+    int s = 0;
+    auto flush = [&] {
+        const int row = s_row[s][m];
+        if (row >= 0) {
+            const float f = s_step[row].s * s_gate[s][m];
+            const f32x4 sw = *reinterpret_cast<const f32x4*>(&s_sw[s][c16 * 4]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * f * sw[i];
+        }
+        acc = i32x4{0, 0, 0, 0};
+    };
+    auto work = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (slot[from][i] >= total) break;
+            if (slot[from][i] != s) {
+                flush();
+                s = slot[from][i];
+            }
+            u32x4 q = {0u, 0u, 0u, 0u};
+            const int row = s_row[s][m];
+            if (row >= 0) {
+                float v[16];
+                raw_values<W8_F32>(raw[from][i], v);
+                q = near_codes16(v, s_step[row].inv);
+            }
+            acc = mfma16_i8(w[from][i], q, acc);
+        }
+    };
+    fetch(0);
+    for (int g = wave; g < units; g += 2 * B * NW) {
+        fetch(1);
+        work(0);
+        fetch(0);
+        work(1);
+    }
+    if (s < total) flush();
     s_part[wave][lane] = y;
     __syncthreads();
+    const int64_t n = (int64_t)blockIdx.x * 16 + c16 * 4;
     if (wave != 0 || m >= a.T || n >= a.H) return;
 #pragma unroll
     for (int i = 1; i < NW; ++i) y += s_part[i][lane];
     const float v[4] = {y[0], y[1], y[2], y[3]};
     store4<BF>(a.Y + m * a.H + n, v, (int)(a.H - n < 4 ? a.H - n : 4), (a.H & 3) == 0);
+}
+template <int IN>
+static int launch_few(const W8FewArgs& a, hipStream_t s) {
+    const int P = a.T * a.topk;
+    const dim3 gu((unsigned)((a.F + 15) / 16), (unsigned)(P < a.E ? P : a.E)), gd((unsigned)((a.H + 15) / 16));
+    // (whole chunks of 128: no piece of 16 columns lies partly or entirely in the padding)
+    if (a.H % 128 == 0) w8_few_up_kernel<IN, true><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
+    else w8_few_up_kernel<IN, false><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
+    const int st = launch_status();
+    if (st != MILO_OK) return st;
+    if (a.F % 128 == 0) w8_few_down_kernel<IN == W8_BF16, true><<<gd, dim3(kFewDownThreads), 0, s>>>(a);
+    else w8_few_down_kernel<IN == W8_BF16, false><<<gd, dim3(kFewDownThreads), 0, s>>>(a);
+    return launch_status();
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -333,19 +410,7 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
         a.h = reinterpret_cast<float*>(ws + L.off_h);
         a.tops = reinterpret_cast<uint32_t*>(ws + L.off_tops);
         a.Y = Y;
-        auto units = [&](int64_t K, int cap) {
-            const int64_t kb = w8_kblocks(K), most = cap / (64 * T);
-            return (int)(kb < most ? kb : most);
-        };
-        const int uu = units(H, kFewUpLds), ud = units(F, kFewDownLds);
-        const dim3 gu((unsigned)((F + 15) / 16), (unsigned)(P < E ? P : E)), gd((unsigned)((H + 15) / 16));
-        if (bf) w8_few_up_kernel<W8_BF16><<<gu, dim3(kFewUpThreads), uu * 64 * (int)T, s>>>(a, uu);
-        else w8_few_up_kernel<W8_F16><<<gu, dim3(kFewUpThreads), uu * 64 * (int)T, s>>>(a, uu);
-        int st = launch_status();
-        if (st != MILO_OK) return st;
-        if (bf) w8_few_down_kernel<true><<<gd, dim3(kFewDownThreads), ud * 64 * (int)T, s>>>(a, ud);
-        else w8_few_down_kernel<false><<<gd, dim3(kFewDownThreads), ud * 64 * (int)T, s>>>(a, ud);
-        return launch_status();
+        return bf ? launch_few<W8_BF16>(a, s) : launch_few<W8_F16>(a, s);
     }
     W8QuantArgs q;
     q.in = X;
