@@ -15,6 +15,11 @@ namespace milo {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void* LdsDst;
+// A pointer that was read from memory (an expert table's) says nothing about its address space, and a load through it would count as an
+// LDS operation too: fragments go through these.
+typedef const __attribute__((address_space(1))) u32x4* GlobalFrag;
+__device__ __forceinline__ GlobalFrag global_frag(const void* p) { return (GlobalFrag)(uintptr_t)p; }
+__device__ __forceinline__ const __attribute__((address_space(1))) float* global_float(const void* p) { return (const __attribute__((address_space(1))) float*)(uintptr_t)p; }
 
 // Columns are padded to whole chunks of 128 (zeros), rows to whole blocks of 16.
 __host__ __device__ inline int64_t w8_kblocks(int64_t K) { return (K + 127) / 128 * 2; }
@@ -48,10 +53,10 @@ __device__ __forceinline__ RowStep row_step(uint32_t top_bits) {
 // of it.  x - c s is a multiple of half a unit in the last place of s and at most about s/2, hence exact in fp32, and
 // comparing it with s/2 settles the code, ties included, without a division.
 __device__ __forceinline__ int row_code(float x, const RowStep& r) {
-    float c = rintf(x * r.inv);
-    const float d = fmaf(-c, r.s, x), far = fabsf(d);
-    if (far >= r.half && (far > r.half || ((int)c & 1))) c += copysignf(1.0f, d);
-    return r.inv > 0.0f ? (int)c : 0;
+    const float c = rintf(x * r.inv), d = fmaf(-c, r.s, x), far = fabsf(d);
+    const int q = (int)c, away = d > 0.0f ? 1 : -1;
+    const bool other = (far > r.half) | ((far == r.half) & ((q & 1) != 0));
+    return r.inv > 0.0f ? q + (other ? away : 0) : 0;
 }
 __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
     return (uint32_t)(a & 255) | (uint32_t)(b & 255) << 8 | (uint32_t)(c & 255) << 16 | (uint32_t)d << 24;

@@ -263,8 +263,7 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
     for (; c < kb; ++c) stage(std::bool_constant<false>{});
     // lane: row (of 32) l32, output features 8 i + 4 h + 0..3
     const bool vec = (a.N & 3) == 0;
-    const float* const sw0 = w8_scales(w0, a.N, a.K);
-    const float* const sw1 = w8_scales(w1, a.N, a.K);
+    const auto sw0 = global_float(w8_scales(w0, a.N, a.K)), sw1 = global_float(w8_scales(w1, a.N, a.K));
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
         const int r = (wm * TM + m) * 32 + l32;

@@ -14,7 +14,7 @@
 namespace milo {
 
 constexpr int kFewTokens = 16, kFewMaxPairs = 128;
-constexpr int kFewUpThreads = 256, kFewDownThreads = 512;
+constexpr int kFewUpThreads = 256, kFewDownThreads = 1024;
 
 struct W8FewArgs {
     const void* X;
@@ -69,13 +69,14 @@ __device__ __forceinline__ int slot_of(const int32_t* s_ids, int topk, int t, in
 }
 
 // Both kernels: column m of an operand of the matrix cores is token m, and lane (m, c) quantizes the 16 values of token m that it
-// holds of it itself, from the row's scale, straight from memory (the rows are small and stay in the caches); a
-// wave works on kFewBatch fragments of the weight at a time, and has the next ones on their way.
-constexpr int kFewBatch = 4;
+// holds of it itself, from the row's scale, straight from memory (the rows are small and stay in the caches).  Waves share
+// the fragments of the weights in runs, 1 KB a fragment, and have the next run on its way.  No branch stands between the loads:
+// what lies past an end is loaded from a clamped place and multiplied with zeros.
+constexpr int kFewUpRun = 2, kFewDownRun = 4;
 
 template <int IN, bool WHOLE>
-__global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArgs a) {
-    constexpr int NW = kFewUpThreads / 64, B = kFewBatch;
+__global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8FewArgs a) {
+    constexpr int NW = kFewUpThreads / 64, B = kFewUpRun;
     __shared__ __attribute__((aligned(16))) int32_t s_ids[kFewMaxPairs];
     __shared__ int32_t s_list[kFewMaxPairs], s_count[NW];
     __shared__ int32_t s_slot[kFewTokens];
@@ -92,18 +93,18 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     const void* const p1 = a.experts[e].w1;
     const void* const p3 = a.experts[e].w3;
     const int64_t wskip = (int64_t)blockIdx.x * kb * 1024;
-    const u32x4* const w1 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p1) + wskip) + lane;
-    const u32x4* const w3 = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(p3) + wskip) + lane;
+    const GlobalFrag w1 = global_frag(reinterpret_cast<const char*>(p1) + wskip) + lane;
+    const GlobalFrag w3 = global_frag(reinterpret_cast<const char*>(p3) + wskip) + lane;
     u32x4 f1[2][B], f3[2][B];
-    auto fetch = [&](int u, int to) {               // fragments u, u + NW, .. (past the end: the last one, for nothing)
+    auto fetch = [&](int u, int to) {
 #pragma unroll
         for (int i = 0; i < B; ++i) {
-            const int v = u + i * NW < kb ? u + i * NW : kb - 1;
-            f1[to][i] = w1[(int64_t)v * 64];
-            f3[to][i] = w3[(int64_t)v * 64];
+            const int v = u + i < kb ? u + i : kb - 1;
+            f1[to][i] = w1[v * 64];
+            f3[to][i] = w3[v * 64];
         }
     };
-    fetch(wave, 0);
+    fetch(wave * B, 0);
     if (tid < kFewTokens) s_slot[tid] = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
     __syncthreads();
     const char* const X = reinterpret_cast<const char*>(a.X);
@@ -117,34 +118,30 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     __syncthreads();
     const int m = lane & 15, c16 = lane >> 4;
     const bool mine = m < a.T && s_slot[m] >= 0;
-    const RowStep step = s_step[m];
+    RowStep step = {0.0f, 0.0f, __uint_as_float(0x7f800000u)};
+    if (mine) step = s_step[m];
     const char* const x = X + (mine ? m : 0) * a.H * 2;
     i32x4 acc1 = {0, 0, 0, 0}, acc3 = {0, 0, 0, 0};
     auto work = [&](int u, int from) {
         W8Raw<IN> raw[B];
-        if (mine) {
 #pragma unroll
-            for (int i = 0; i < B; ++i)
-                if (u + i * NW < kb) raw[i] = load16<IN, WHOLE>(x, (int64_t)(u + i * NW) * 64 + c16 * 16, a.H);
-        }
+        for (int i = 0; i < B; ++i) raw[i] = load16<IN, WHOLE>(x, (u + i < kb ? u + i : kb - 1) * 64 + c16 * 16, a.H);
+        fetch(u + B * NW, from ^ 1);
+        asm volatile("" ::: "memory");              // (the loads stay in front)
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < B; ++i) {
-            if (u + i * NW >= kb) break;
-            u32x4 q = {0u, 0u, 0u, 0u};
-            if (mine) {
-                float v[16];
-                raw_values<IN>(raw[i], v);
-                q = row_codes16(v, step);
-            }
+            float v[16];
+            raw_values<IN>(raw[i], v);
+            u32x4 q = row_codes16(v, step);
+            if (!mine || u + i >= kb) q = u32x4{0u, 0u, 0u, 0u};
             acc1 = mfma16_i8(f1[from][i], q, acc1);
             acc3 = mfma16_i8(f3[from][i], q, acc3);
         }
     };
-    for (int u = wave; u < kb; u += 2 * B * NW) {
-        fetch(u + B * NW, 1);
+    for (int u = wave * B; u < kb; u += 2 * B * NW) {
         work(u, 0);
         if (u + B * NW >= kb) break;
-        fetch(u + 2 * B * NW, 0);
         work(u + B * NW, 1);
     }
     s_part[0][wave][lane] = acc1;
@@ -160,8 +157,7 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     uint32_t top = 0u;
     const int64_t row = mine ? m * a.topk + s_slot[m] : 0;
     if (mine) {
-        const float* const sw1 = w8_scales(p1, a.F, a.H) + n;
-        const float* const sw3 = w8_scales(p3, a.F, a.H) + n;
+        const auto sw1 = global_float(w8_scales(p1, a.F, a.H) + n), sw3 = global_float(w8_scales(p3, a.F, a.H) + n);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (n + i >= a.F) continue;
@@ -179,23 +175,45 @@ __global__ __launch_bounds__(kFewUpThreads) void w8_few_up_kernel(const W8FewArg
     if (mine && c16 == 0) a.tops[row * ((a.F + 15) / 16) + blockIdx.x] = top;
 }
 
-// The fragments of all experts' weights are one sequence, which the waves share; a wave adds up an expert's products
-// in integers and turns to fp32 where it goes on to the next expert.
-template <bool BF, bool WHOLE>
-__global__ __launch_bounds__(kFewDownThreads) void w8_few_down_kernel(const W8FewArgs a) {
-    constexpr int NW = kFewDownThreads / 64, B = kFewBatch;
+// The runs of all experts' weights are one sequence, which the waves share; the products of a run are added up in integers and
+// turned to fp32 at its end.  (A row of H is read past its end where the weight's codes are padding, that is zero.)
+template <bool BF>
+__global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W8FewArgs a) {
+    constexpr int NW = kFewDownThreads / 64, B = kFewDownRun;
+    struct Lane {
+        uint32_t off;       // of the token's row of H in bytes, or out of range
+        float inv, f;       // 1 / its scale;  its scale times the gate
+    };
     __shared__ __attribute__((aligned(16))) int32_t s_ids[kFewMaxPairs];
     __shared__ int32_t s_list[kFewMaxPairs], s_count[NW];
     __shared__ RowStep s_step[kFewMaxPairs];                        // per pair
-    __shared__ const void* s_w[kFewMaxPairs];                       // per expert that occurs: its weight,
-    __shared__ float s_sw[kFewMaxPairs][16];                        // the scales of this workgroup's features,
-    __shared__ int16_t s_row[kFewMaxPairs][kFewTokens];             // the tokens' rows of H (-1: none)
-    __shared__ float s_gate[kFewMaxPairs][kFewTokens];              // and their weights
+    __shared__ uint64_t s_w[kFewMaxPairs];                          // per expert that occurs: its weight,
+    __shared__ __attribute__((aligned(16))) float s_sw[kFewMaxPairs][16];   // the scales of this workgroup's features,
+    __shared__ Lane s_lane[kFewMaxPairs][kFewTokens];               // and its tokens
     __shared__ f32x4 s_part[NW][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kb = (int)w8_kblocks(a.F), nt = (int)((a.F + 15) / 16), P = a.T * a.topk;
     bool bad;
     const int total = distinct_experts<kFewDownThreads>(a, s_ids, s_list, s_count, &bad);
+    for (int i = tid; i < total * 16; i += kFewDownThreads) {
+        const int s = i >> 4;
+        const void* const w = a.experts[s_list[s]].w2;
+        if ((i & 15) == 0) s_w[s] = (uint64_t)(uintptr_t)w;
+        s_sw[s][i & 15] = global_float(w8_scales(w, a.H, a.F))[(int64_t)blockIdx.x * 16 + (i & 15)];
+    }
+    __syncthreads();
+    // run r: fragments B (r % runs) .. of expert r / runs
+    const int runs = (kb + B - 1) / B, all = total * runs;
+    const int64_t skip = (int64_t)blockIdx.x * kb * 64 + lane;
+    u32x4 w[2][B];
+    auto fetch = [&](int r, int to) {
+        r = r < all ? r : all - 1;
+        const int s = r / runs, u = (r - s * runs) * B;
+        const GlobalFrag p = global_frag((const void*)(uintptr_t)s_w[s]) + skip;
+#pragma unroll
+        for (int i = 0; i < B; ++i) w[to][i] = p[(u + i < kb ? u + i : kb - 1) * 64];
+    };
+    if (total > 0) fetch(wave, 0);
     for (int p = wave; p < P; p += NW) {
         if (s_ids[p] < 0) continue;
         uint32_t top = 0u;
@@ -204,81 +222,58 @@ __global__ __launch_bounds__(kFewDownThreads) void w8_few_down_kernel(const W8Fe
         top = wave_max(top);
         if (lane == 0) s_step[p] = row_step(top);
     }
+    __syncthreads();
     for (int i = tid; i < total * 16; i += kFewDownThreads) {
         const int s = i >> 4, m = i & 15, e = s_list[s];
-        const void* const w = a.experts[e].w2;
-        if (m == 0) s_w[s] = w;
-        s_sw[s][m] = w8_scales(w, a.H, a.F)[(int64_t)blockIdx.x * 16 + m];
         const int j = m < a.T ? slot_of(s_ids, a.topk, m, e) : -1;
-        float g = 0.0f;
-        if (j >= 0)
+        Lane l = {kOobOffset, 0.0f, 0.0f};
+        if (j >= 0) {
+            float g = 0.0f;
             for (int k = 0; k < a.topk; ++k) g += s_ids[m * a.topk + k] == e ? a.gates[m * a.topk + k] : 0.0f;
-        s_row[s][m] = (int16_t)(j >= 0 ? m * a.topk + j : -1);
-        s_gate[s][m] = g;
+            const int row = m * a.topk + j;
+            l.off = (uint32_t)row * (uint32_t)a.F * 4u;
+            l.inv = s_step[row].inv;
+            l.f = s_step[row].s * g;
+        }
+        s_lane[s][m] = l;
     }
     __syncthreads();
-    const int m = lane & 15, c16 = lane >> 4, units = total * kb;
-    const int64_t skip = (int64_t)blockIdx.x * kb * 64 + lane;
+    const int m = lane & 15, c16 = lane >> 4;
+    const BufRsrc rh = make_rsrc(a.h, (uint64_t)P * (uint64_t)a.F * 4u);
     f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-    i32x4 acc = {0, 0, 0, 0};
-    // unit g: fragment g % kb of expert g / kb.  One batch of units: of which expert and fragment, its weight and its rows of H
-    int slot[2][B];
-    u32x4 w[2][B];
-    W8Raw<W8_F32> raw[2][B];
-    int fs = 0, fu = wave;                          // the next unit to fetch
-    auto fetch = [&](int to) {
+    auto work = [&](int r, int from) {
+        const int s = r / runs, u = (r - s * runs) * B;
+        const Lane l = s_lane[s][m];
+        const f32x4 sw = *reinterpret_cast<const f32x4*>(&s_sw[s][c16 * 4]);
+        u32x4 raw[B][4];
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t o = l.off == kOobOffset ? kOobOffset : l.off + (uint32_t)((u + i) * 256 + c16 * 64 + j * 16);
+                raw[i][j] = buf_load16(rh, o);
+            }
+        fetch(r + NW, from ^ 1);
+        asm volatile("" ::: "memory");              // (the loads stay in front)
+        __builtin_amdgcn_sched_barrier(0);
+        i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < B; ++i) {
-            while (fu >= kb) {
-                fu -= kb;
-                ++fs;
-            }
-            slot[to][i] = fs;
-            if (fs < total) {
-                w[to][i] = (reinterpret_cast<const u32x4*>(s_w[fs]) + skip)[(int64_t)fu * 64];
-                const int row = s_row[fs][m];
-                if (row >= 0) raw[to][i] = load16<W8_F32, WHOLE>(a.h + (int64_t)row * a.F, (int64_t)fu * 64 + c16 * 16, a.F);
-            }
-            fu += NW;
-        }
-    };
-    int s = 0;
-    auto flush = [&] {
-        const int row = s_row[s][m];
-        if (row >= 0) {
-            const float f = s_step[row].s * s_gate[s][m];
-            const f32x4 sw = *reinterpret_cast<const f32x4*>(&s_sw[s][c16 * 4]);
+            float v[16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * f * sw[i];
-        }
-        acc = i32x4{0, 0, 0, 0};
-    };
-    auto work = [&](int from) {
-#pragma unroll
-        for (int i = 0; i < B; ++i) {
-            if (slot[from][i] >= total) break;
-            if (slot[from][i] != s) {
-                flush();
-                s = slot[from][i];
-            }
-            u32x4 q = {0u, 0u, 0u, 0u};
-            const int row = s_row[s][m];
-            if (row >= 0) {
-                float v[16];
-                raw_values<W8_F32>(raw[from][i], v);
-                q = near_codes16(v, s_step[row].inv);
-            }
+            for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(raw[i][j >> 2][j & 3]);
+            u32x4 q = near_codes16(v, l.inv);
+            if (u + i >= kb) q = u32x4{0u, 0u, 0u, 0u};
             acc = mfma16_i8(w[from][i], q, acc);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * l.f * sw[i];
     };
-    fetch(0);
-    for (int g = wave; g < units; g += 2 * B * NW) {
-        fetch(1);
-        work(0);
-        fetch(0);
-        work(1);
+    for (int r = wave; r < all; r += 2 * NW) {
+        work(r, 0);
+        if (r + NW >= all) break;
+        work(r + NW, 1);
     }
-    if (s < total) flush();
     s_part[wave][lane] = y;
     __syncthreads();
     const int64_t n = (int64_t)blockIdx.x * 16 + c16 * 4;
@@ -297,8 +292,7 @@ static int launch_few(const W8FewArgs& a, hipStream_t s) {
     else w8_few_up_kernel<IN, false><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
     const int st = launch_status();
     if (st != MILO_OK) return st;
-    if (a.F % 128 == 0) w8_few_down_kernel<IN == W8_BF16, true><<<gd, dim3(kFewDownThreads), 0, s>>>(a);
-    else w8_few_down_kernel<IN == W8_BF16, false><<<gd, dim3(kFewDownThreads), 0, s>>>(a);
+    w8_few_down_kernel<IN == W8_BF16><<<gd, dim3(kFewDownThreads), 0, s>>>(a);
     return launch_status();
 }
 
