@@ -26,8 +26,11 @@ struct W8FewArgs {
     int32_t* status;        // routing status
     float* h;               // [pairs x F]
     uint32_t* tops;         // [pairs x ceil(F/16)] largest magnitude of 16 features of H, fp32 bits
+    uint8_t* hcodes;        // the rows of H quantized (where the down projection does not do it itself), row-major, and their scales
+    float* hscales;
     uint16_t* Y;
 };
+constexpr int kFewStagedBytes = 64 * 1024;      // most codes that the down projection holds in LDS
 
 // The experts that occur in the ids, in the order of their first occurrence: their number, and in list[i] the i-th
 // one's id.  All threads of the workgroup take part; s_ids receives the ids, -1 for one out of range.
@@ -176,98 +179,115 @@ __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8Few
 }
 
 // The runs of all experts' weights are one sequence, which the waves share; the products of a run are added up in integers and
-// turned to fp32 at its end.  (A row of H is read past its end where the weight's codes are padding, that is zero.)
-template <bool BF>
+// turned to fp32 at its end.  STAGED: the codes of all rows fit LDS, and the workgroup forms them there from fp32 rows; else a
+// launch of the row quantizer has formed them (every workgroup would read all rows, four times the codes' bytes).
+template <bool BF, bool STAGED>
 __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W8FewArgs a) {
     constexpr int NW = kFewDownThreads / 64, B = kFewDownRun;
-    struct Lane {
-        uint32_t off;       // of the token's row of H in bytes, or out of range
-        float inv, f;       // 1 / its scale;  its scale times the gate
-    };
     __shared__ __attribute__((aligned(16))) int32_t s_ids[kFewMaxPairs];
     __shared__ int32_t s_list[kFewMaxPairs], s_count[NW];
-    __shared__ RowStep s_step[kFewMaxPairs];                        // per pair
+    __shared__ RowStep s_step[STAGED ? kFewMaxPairs : 1];           // per pair
     __shared__ uint64_t s_w[kFewMaxPairs];                          // per expert that occurs: its weight,
     __shared__ __attribute__((aligned(16))) float s_sw[kFewMaxPairs][16];   // the scales of this workgroup's features,
-    __shared__ Lane s_lane[kFewMaxPairs][kFewTokens];               // and its tokens
+    __shared__ int32_t s_row[kFewMaxPairs][kFewTokens];             // its tokens' rows (-1: none)
+    __shared__ float s_factor[kFewMaxPairs][kFewTokens];            // and the rows' scales times the gates
     __shared__ f32x4 s_part[NW][64];
+    extern __shared__ __attribute__((aligned(16))) unsigned char codes[];   // piece c of 16 columns of pair p: at (c * P + p) * 16
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kb = (int)w8_kblocks(a.F), nt = (int)((a.F + 15) / 16), P = a.T * a.topk;
+    const int kb = (int)w8_kblocks(a.F), P = a.T * a.topk;
+    if constexpr (STAGED) {
+        const int nt = (int)((a.F + 15) / 16);
+        for (int p = wave; p < P; p += NW) {        // (a pair that has no row: some value, which nothing uses)
+            uint32_t top = 0u;
+            const uint32_t* const tops = a.tops + (int64_t)p * nt;
+            for (int i = lane; i < nt; i += 64) top = tops[i] > top ? tops[i] : top;
+            top = wave_max(top);
+            if (lane == 0) s_step[p] = row_step(top);
+        }
+    }
     bool bad;
     const int total = distinct_experts<kFewDownThreads>(a, s_ids, s_list, s_count, &bad);
     for (int i = tid; i < total * 16; i += kFewDownThreads) {
-        const int s = i >> 4;
-        const void* const w = a.experts[s_list[s]].w2;
-        if ((i & 15) == 0) s_w[s] = (uint64_t)(uintptr_t)w;
-        s_sw[s][i & 15] = global_float(w8_scales(w, a.H, a.F))[(int64_t)blockIdx.x * 16 + (i & 15)];
+        const int s = i >> 4, m = i & 15, e = s_list[s];
+        const void* const w = a.experts[e].w2;
+        if (m == 0) s_w[s] = (uint64_t)(uintptr_t)w;
+        s_sw[s][m] = global_float(w8_scales(w, a.H, a.F))[(int64_t)blockIdx.x * 16 + m];
+        const int j = m < a.T ? slot_of(s_ids, a.topk, m, e) : -1, row = j >= 0 ? m * a.topk + j : -1;
+        float f = 0.0f;
+        if (j >= 0) {
+            for (int k = j; k < a.topk; ++k) f += s_ids[m * a.topk + k] == e ? a.gates[m * a.topk + k] : 0.0f;
+            f *= STAGED ? s_step[row].s : a.hscales[row];
+        }
+        s_row[s][m] = row;
+        s_factor[s][m] = f;
     }
     __syncthreads();
     // run r: fragments B (r % runs) .. of expert r / runs
+    const int m = lane & 15, c16 = lane >> 4;
     const int runs = (kb + B - 1) / B, all = total * runs;
     const int64_t skip = (int64_t)blockIdx.x * kb * 64 + lane;
-    u32x4 w[2][B];
+    const BufRsrc rq = make_rsrc(a.hcodes, STAGED ? 0 : (uint64_t)P * kb * 64);
+    u32x4 w[2][B], q[2][B];
     auto fetch = [&](int r, int to) {
         r = r < all ? r : all - 1;
         const int s = r / runs, u = (r - s * runs) * B;
         const GlobalFrag p = global_frag((const void*)(uintptr_t)s_w[s]) + skip;
 #pragma unroll
         for (int i = 0; i < B; ++i) w[to][i] = p[(u + i < kb ? u + i : kb - 1) * 64];
-    };
-    if (total > 0) fetch(wave, 0);
-    for (int p = wave; p < P; p += NW) {
-        if (s_ids[p] < 0) continue;
-        uint32_t top = 0u;
-        const uint32_t* const tops = a.tops + (int64_t)p * nt;
-        for (int i = lane; i < nt; i += 64) top = tops[i] > top ? tops[i] : top;
-        top = wave_max(top);
-        if (lane == 0) s_step[p] = row_step(top);
-    }
-    __syncthreads();
-    for (int i = tid; i < total * 16; i += kFewDownThreads) {
-        const int s = i >> 4, m = i & 15, e = s_list[s];
-        const int j = m < a.T ? slot_of(s_ids, a.topk, m, e) : -1;
-        Lane l = {kOobOffset, 0.0f, 0.0f};
-        if (j >= 0) {
-            float g = 0.0f;
-            for (int k = 0; k < a.topk; ++k) g += s_ids[m * a.topk + k] == e ? a.gates[m * a.topk + k] : 0.0f;
-            const int row = m * a.topk + j;
-            l.off = (uint32_t)row * (uint32_t)a.F * 4u;
-            l.inv = s_step[row].inv;
-            l.f = s_step[row].s * g;
+        if constexpr (!STAGED) {
+            const int row = s_row[s][m];
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                const uint32_t o = row >= 0 && u + i < kb ? (uint32_t)row * (uint32_t)(kb * 64) + (uint32_t)((u + i) * 64 + c16 * 16) : kOobOffset;
+                q[to][i] = buf_load16(rq, o);
+            }
         }
-        s_lane[s][m] = l;
+    };
+    if (all > 0) fetch(wave, 0);
+    if constexpr (STAGED) {
+        // four values a thread: neighbours are the quarters of a piece, then the pairs
+        const int n = P * kb * 16;
+#pragma unroll 4
+        for (int i = tid; i < n; i += kFewDownThreads) {
+            const int c = (i >> 2) / P, p = (i >> 2) - c * P;
+            const int64_t k = (int64_t)c * 16 + (i & 3) * 4;
+            const float* const h = a.h + (int64_t)p * a.F + k;
+            float v[4];
+            if (k + 4 <= a.F) {
+                __builtin_memcpy(v, h, 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = k + j < a.F ? h[j] : 0.0f;
+            }
+            uint32_t b[4];
+            const float inv = s_step[p].inv;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(fmaf(v[j], inv, kRoundMagic));
+            *reinterpret_cast<uint32_t*>(codes + i * 4) = low_bytes(b[0], b[1], b[2], b[3]);
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    const int m = lane & 15, c16 = lane >> 4;
-    const BufRsrc rh = make_rsrc(a.h, (uint64_t)P * (uint64_t)a.F * 4u);
     f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
     auto work = [&](int r, int from) {
         const int s = r / runs, u = (r - s * runs) * B;
-        const Lane l = s_lane[s][m];
+        const float f = s_factor[s][m];
         const f32x4 sw = *reinterpret_cast<const f32x4*>(&s_sw[s][c16 * 4]);
-        u32x4 raw[B][4];
+        if constexpr (STAGED) {
+            const int row = s_row[s][m];
 #pragma unroll
-        for (int i = 0; i < B; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t o = l.off == kOobOffset ? kOobOffset : l.off + (uint32_t)((u + i) * 256 + c16 * 64 + j * 16);
-                raw[i][j] = buf_load16(rh, o);
+            for (int i = 0; i < B; ++i) {
+                q[from][i] = *reinterpret_cast<const u32x4*>(codes + (((u + i < kb ? u + i : 0) * 4 + c16) * P + (row >= 0 ? row : 0)) * 16);
+                if (row < 0 || u + i >= kb) q[from][i] = u32x4{0u, 0u, 0u, 0u};
             }
+        }
         fetch(r + NW, from ^ 1);
         asm volatile("" ::: "memory");              // (the loads stay in front)
         __builtin_amdgcn_sched_barrier(0);
         i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-            float v[16];
+        for (int i = 0; i < B; ++i) acc = mfma16_i8(w[from][i], q[from][i], acc);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(raw[i][j >> 2][j & 3]);
-            u32x4 q = near_codes16(v, l.inv);
-            if (u + i >= kb) q = u32x4{0u, 0u, 0u, 0u};
-            acc = mfma16_i8(w[from][i], q, acc);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * l.f * sw[i];
+        for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * f * sw[i];
     };
     for (int r = wave; r < all; r += 2 * NW) {
         work(r, 0);
@@ -283,6 +303,21 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
     const float v[4] = {y[0], y[1], y[2], y[3]};
     store4<BF>(a.Y + m * a.H + n, v, (int)(a.H - n < 4 ? a.H - n : 4), (a.H & 3) == 0);
 }
+template <bool BF, bool STAGED>
+static int launch_few_down(const W8FewArgs& a, dim3 grid, int lds, hipStream_t stream) {
+    if constexpr (STAGED) {
+        static bool raised[64] = {false};
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MILO_ERR_HIP;
+        if (!raised[dev]) {
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_few_down_kernel<BF, STAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewStagedBytes) != hipSuccess)
+                return MILO_ERR_HIP;
+            raised[dev] = true;
+        }
+    }
+    w8_few_down_kernel<BF, STAGED><<<grid, dim3(kFewDownThreads), lds, stream>>>(a);
+    return launch_status();
+}
 template <int IN>
 static int launch_few(const W8FewArgs& a, hipStream_t s) {
     const int P = a.T * a.topk;
@@ -290,10 +325,20 @@ static int launch_few(const W8FewArgs& a, hipStream_t s) {
     // (whole chunks of 128: no piece of 16 columns lies partly or entirely in the padding)
     if (a.H % 128 == 0) w8_few_up_kernel<IN, true><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
     else w8_few_up_kernel<IN, false><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
-    const int st = launch_status();
+    int st = launch_status();
     if (st != MILO_OK) return st;
-    w8_few_down_kernel<IN == W8_BF16><<<gd, dim3(kFewDownThreads), 0, s>>>(a);
-    return launch_status();
+    const int bytes = P * (int)w8_kblocks(a.F) * 64;
+    if (bytes <= kFewStagedBytes) return launch_few_down<IN == W8_BF16, true>(a, gd, bytes, s);
+    W8QuantArgs q;
+    q.in = a.h;
+    q.rows = P;
+    q.K = a.F;
+    q.codes = a.hcodes;
+    q.scales = a.hscales;
+    q.blocked = 0;
+    st = launch_w8_quant(q, W8_F32, s);
+    if (st != MILO_OK) return st;
+    return launch_few_down<IN == W8_BF16, false>(a, gd, 0, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -341,6 +386,8 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     L->off_h = take((size_t)P * F * 4);
     if (L->few) {
         L->off_tops = take((size_t)P * ((F + 15) / 16) * 4);
+        L->off_hq = take((size_t)(P * fb));
+        L->off_hs = take((size_t)P * 4);
     } else {
         L->bm = P >= 192 * (int64_t)E ? 256 : 128;
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
@@ -403,6 +450,8 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
         a.status = status;
         a.h = reinterpret_cast<float*>(ws + L.off_h);
         a.tops = reinterpret_cast<uint32_t*>(ws + L.off_tops);
+        a.hcodes = reinterpret_cast<uint8_t*>(ws + L.off_hq);
+        a.hscales = reinterpret_cast<float*>(ws + L.off_hs);
         a.Y = Y;
         return bf ? launch_few<W8_BF16>(a, s) : launch_few<W8_F16>(a, s);
     }
