@@ -26,11 +26,11 @@ struct W8FewArgs {
     int32_t* status;        // routing status
     float* h;               // [pairs x F]
     uint32_t* tops;         // [pairs x ceil(F/16)] largest magnitude of 16 features of H, fp32 bits
-    uint8_t* hcodes;        // the rows of H quantized (where the down projection does not do it itself), row-major, and their scales
-    float* hscales;
+    uint8_t *xcodes, *hcodes;       // X and H quantized (where the products do not do it themselves), row-major, and their scales
+    float *xscales, *hscales;
     uint16_t* Y;
 };
-constexpr int kFewStagedBytes = 64 * 1024;      // most codes that the down projection holds in LDS
+constexpr int kFewUpStaged = 16 * 1024, kFewDownStaged = 64 * 1024;      // most codes that the products form and hold in LDS
 
 // The experts that occur in the ids, in the order of their first occurrence: their number, and in list[i] the i-th
 // one's id.  All threads of the workgroup take part; s_ids receives the ids, -1 for one out of range.
@@ -71,20 +71,22 @@ __device__ __forceinline__ int slot_of(const int32_t* s_ids, int topk, int t, in
     return found;
 }
 
-// Both kernels: column m of an operand of the matrix cores is token m, and lane (m, c) quantizes the 16 values of token m that it
-// holds of it itself, from the row's scale, straight from memory (the rows are small and stay in the caches).  Waves share
-// the fragments of the weights in runs, 1 KB a fragment, and have the next run on its way.  No branch stands between the loads:
-// what lies past an end is loaded from a clamped place and multiplied with zeros.
+// Both kernels: column m of an operand of the matrix cores is token m.  Waves share the fragments of the weights in runs, 1 KB a
+// fragment, and have the next run on its way.  No branch stands between the loads: what lies past an end is loaded from a
+// clamped place and multiplied with zeros.  STAGED: the codes of the rows fit LDS, and the workgroup forms them there (so the
+// layer takes two launches); else a launch of the row quantizer has formed them (every workgroup reads all of its rows, so the
+// saving grows with the tokens).
 constexpr int kFewUpRun = 2, kFewDownRun = 4;
 
-template <int IN, bool WHOLE>
+template <int IN, bool STAGED>
 __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8FewArgs a) {
     constexpr int NW = kFewUpThreads / 64, B = kFewUpRun;
     __shared__ __attribute__((aligned(16))) int32_t s_ids[kFewMaxPairs];
     __shared__ int32_t s_list[kFewMaxPairs], s_count[NW];
     __shared__ int32_t s_slot[kFewTokens];
-    __shared__ RowStep s_step[kFewTokens];
+    __shared__ uint32_t s_top[STAGED ? kFewTokens : 1][NW];
     __shared__ i32x4 s_part[2][NW][64];
+    extern __shared__ __attribute__((aligned(16))) unsigned char codes[];   // piece c of 16 columns of token t: at (c * T + t) * 16
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int slot = blockIdx.y;
     bool bad;
@@ -95,51 +97,80 @@ __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8Few
     const int kb = (int)w8_kblocks(a.H);
     const void* const p1 = a.experts[e].w1;
     const void* const p3 = a.experts[e].w3;
+    if (tid < kFewTokens) s_slot[tid] = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
+    __syncthreads();
+    const int m = lane & 15, c16 = lane >> 4;
+    const bool mine = s_slot[m] >= 0;
     const int64_t wskip = (int64_t)blockIdx.x * kb * 1024;
     const GlobalFrag w1 = global_frag(reinterpret_cast<const char*>(p1) + wskip) + lane;
     const GlobalFrag w3 = global_frag(reinterpret_cast<const char*>(p3) + wskip) + lane;
-    u32x4 f1[2][B], f3[2][B];
+    const BufRsrc rq = make_rsrc(a.xcodes, STAGED ? 0 : (uint64_t)a.T * kb * 64);
+    u32x4 f1[2][B], f3[2][B], q[2][B];
     auto fetch = [&](int u, int to) {
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             const int v = u + i < kb ? u + i : kb - 1;
             f1[to][i] = w1[v * 64];
             f3[to][i] = w3[v * 64];
+            if constexpr (!STAGED) {
+                const uint32_t o = mine && u + i < kb ? (uint32_t)(m * kb * 64 + (u + i) * 64 + c16 * 16) : kOobOffset;
+                q[to][i] = buf_load16(rq, o);
+            }
         }
     };
     fetch(wave * B, 0);
-    if (tid < kFewTokens) s_slot[tid] = tid < a.T ? slot_of(s_ids, a.topk, tid, e) : -1;
-    __syncthreads();
-    const char* const X = reinterpret_cast<const char*>(a.X);
-    for (int t = wave; t < a.T; t += NW) {
-        if (s_slot[t] < 0) continue;
-        uint32_t top = 0u;
-        for (int p = lane; p < (int)((a.H + 15) / 16); p += 64) top = raw_top<IN>(load16<IN, WHOLE>(X + t * a.H * 2, (int64_t)p * 16, a.H), top);
-        top = wave_max(top);
-        if (lane == 0) s_step[t] = row_step(top);
+    if constexpr (STAGED) {
+        const char* const X = reinterpret_cast<const char*>(a.X);
+        const int pieces = kb * 4;
+        for (int t = 0; t < a.T; ++t) {
+            if (s_slot[t] < 0) continue;
+            uint32_t top = 0u;
+            for (int p = tid; p < pieces; p += kFewUpThreads) top = raw_top<IN>(load16<IN>(X + t * a.H * 2, (int64_t)p * 16, a.H), top);
+            top = wave_max(top);
+            if (lane == 0) s_top[t][wave] = top;
+        }
+        __syncthreads();
+        for (int t = 0; t < a.T; ++t) {
+            if (s_slot[t] < 0) continue;
+            uint32_t top = s_top[t][0];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = s_top[t][w] > top ? s_top[t][w] : top;
+            const RowStep st = row_step(top);
+            for (int p = tid; p < pieces; p += kFewUpThreads) {
+                float v[16];
+                raw_values<IN>(load16<IN>(X + t * a.H * 2, (int64_t)p * 16, a.H), v);
+                *reinterpret_cast<u32x4*>(codes + (p * a.T + t) * 16) = row_codes16(v, st);
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    const int m = lane & 15, c16 = lane >> 4;
-    const bool mine = m < a.T && s_slot[m] >= 0;
-    RowStep step = {0.0f, 0.0f, __uint_as_float(0x7f800000u)};
-    if (mine) step = s_step[m];
-    const char* const x = X + (mine ? m : 0) * a.H * 2;
+    float sx = 0.0f;
+    if constexpr (STAGED) {
+        if (mine) {
+            uint32_t top = s_top[m][0];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = s_top[m][w] > top ? s_top[m][w] : top;
+            sx = row_step(top).s;
+        }
+    } else {
+        if (mine) sx = a.xscales[m];
+    }
     i32x4 acc1 = {0, 0, 0, 0}, acc3 = {0, 0, 0, 0};
     auto work = [&](int u, int from) {
-        W8Raw<IN> raw[B];
+        if constexpr (STAGED) {
 #pragma unroll
-        for (int i = 0; i < B; ++i) raw[i] = load16<IN, WHOLE>(x, (u + i < kb ? u + i : kb - 1) * 64 + c16 * 16, a.H);
+            for (int i = 0; i < B; ++i) {
+                q[from][i] = *reinterpret_cast<const u32x4*>(codes + (((u + i < kb ? u + i : 0) * 4 + c16) * a.T + (mine ? m : 0)) * 16);
+                if (!mine || u + i >= kb) q[from][i] = u32x4{0u, 0u, 0u, 0u};
+            }
+        }
         fetch(u + B * NW, from ^ 1);
         asm volatile("" ::: "memory");              // (the loads stay in front)
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < B; ++i) {
-            float v[16];
-            raw_values<IN>(raw[i], v);
-            u32x4 q = row_codes16(v, step);
-            if (!mine || u + i >= kb) q = u32x4{0u, 0u, 0u, 0u};
-            acc1 = mfma16_i8(f1[from][i], q, acc1);
-            acc3 = mfma16_i8(f3[from][i], q, acc3);
+            acc1 = mfma16_i8(f1[from][i], q[from][i], acc1);
+            acc3 = mfma16_i8(f3[from][i], q[from][i], acc3);
         }
     };
     for (int u = wave * B; u < kb; u += 2 * B * NW) {
@@ -164,7 +195,7 @@ __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8Few
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (n + i >= a.F) continue;
-            const float v = silu_times((float)acc1[i] * step.s * sw1[i], (float)acc3[i] * step.s * sw3[i]);
+            const float v = silu_times((float)acc1[i] * sx * sw1[i], (float)acc3[i] * sx * sw3[i]);
             a.h[row * a.F + n + i] = v;
             const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
             top = b > top ? b : top;
@@ -179,8 +210,7 @@ __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8Few
 }
 
 // The runs of all experts' weights are one sequence, which the waves share; the products of a run are added up in integers and
-// turned to fp32 at its end.  STAGED: the codes of all rows fit LDS, and the workgroup forms them there from fp32 rows; else a
-// launch of the row quantizer has formed them (every workgroup would read all rows, four times the codes' bytes).
+// turned to fp32 at its end.
 template <bool BF, bool STAGED>
 __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W8FewArgs a) {
     constexpr int NW = kFewDownThreads / 64, B = kFewDownRun;
@@ -310,7 +340,7 @@ static int launch_few_down(const W8FewArgs& a, dim3 grid, int lds, hipStream_t s
         int dev = 0;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MILO_ERR_HIP;
         if (!raised[dev]) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_few_down_kernel<BF, STAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewStagedBytes) != hipSuccess)
+            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_few_down_kernel<BF, STAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewDownStaged) != hipSuccess)
                 return MILO_ERR_HIP;
             raised[dev] = true;
         }
@@ -322,20 +352,30 @@ template <int IN>
 static int launch_few(const W8FewArgs& a, hipStream_t s) {
     const int P = a.T * a.topk;
     const dim3 gu((unsigned)((a.F + 15) / 16), (unsigned)(P < a.E ? P : a.E)), gd((unsigned)((a.H + 15) / 16));
-    // (whole chunks of 128: no piece of 16 columns lies partly or entirely in the padding)
-    if (a.H % 128 == 0) w8_few_up_kernel<IN, true><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
-    else w8_few_up_kernel<IN, false><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
+    W8QuantArgs q;
+    q.blocked = 0;
+    const int xbytes = a.T * (int)w8_kblocks(a.H) * 64;
+    if (xbytes <= kFewUpStaged) {
+        w8_few_up_kernel<IN, true><<<gu, dim3(kFewUpThreads), xbytes, s>>>(a);
+    } else {
+        q.in = a.X;
+        q.rows = a.T;
+        q.K = a.H;
+        q.codes = a.xcodes;
+        q.scales = a.xscales;
+        const int st = launch_w8_quant(q, IN, s);
+        if (st != MILO_OK) return st;
+        w8_few_up_kernel<IN, false><<<gu, dim3(kFewUpThreads), 0, s>>>(a);
+    }
     int st = launch_status();
     if (st != MILO_OK) return st;
     const int bytes = P * (int)w8_kblocks(a.F) * 64;
-    if (bytes <= kFewStagedBytes) return launch_few_down<IN == W8_BF16, true>(a, gd, bytes, s);
-    W8QuantArgs q;
+    if (bytes <= kFewDownStaged) return launch_few_down<IN == W8_BF16, true>(a, gd, bytes, s);
     q.in = a.h;
     q.rows = P;
     q.K = a.F;
     q.codes = a.hcodes;
     q.scales = a.hscales;
-    q.blocked = 0;
     st = launch_w8_quant(q, W8_F32, s);
     if (st != MILO_OK) return st;
     return launch_few_down<IN == W8_BF16, false>(a, gd, 0, s);
@@ -384,6 +424,8 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     };
     L->few = T <= kFewTokens && P <= kFewMaxPairs;
     L->off_h = take((size_t)P * F * 4);
+    L->off_xq = take((size_t)(T * hb));
+    L->off_xs = take((size_t)T * 4);
     if (L->few) {
         L->off_tops = take((size_t)P * ((F + 15) / 16) * 4);
         L->off_hq = take((size_t)(P * fb));
@@ -391,8 +433,6 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     } else {
         L->bm = P >= 192 * (int64_t)E ? 256 : 128;
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
-        L->off_xq = take((size_t)(T * hb));
-        L->off_xs = take((size_t)T * 4);
         L->off_sorted = take((size_t)P * 4);
         L->off_token = take((size_t)P * 4);
         L->off_tiles = take((size_t)L->max_tiles * sizeof(TileDesc));
@@ -450,6 +490,8 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
         a.status = status;
         a.h = reinterpret_cast<float*>(ws + L.off_h);
         a.tops = reinterpret_cast<uint32_t*>(ws + L.off_tops);
+        a.xcodes = reinterpret_cast<uint8_t*>(ws + L.off_xq);
+        a.xscales = reinterpret_cast<float*>(ws + L.off_xs);
         a.hcodes = reinterpret_cast<uint8_t*>(ws + L.off_hq);
         a.hscales = reinterpret_cast<float*>(ws + L.off_hs);
         a.Y = Y;
