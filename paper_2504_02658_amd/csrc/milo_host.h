@@ -56,6 +56,17 @@ inline int launch_status() {
     return e == hipSuccess ? MILO_OK : MILO_ERR_HIP;
 }
 
+// Lets a kernel have `bytes` of dynamic LDS (more than 64 KB); once per kernel and device, which `raised` remembers.
+inline int raise_lds(const void* kernel, int bytes, bool (&raised)[64]) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MILO_ERR_HIP;
+    if (!raised[dev]) {
+        if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return MILO_ERR_HIP;
+        raised[dev] = true;
+    }
+    return MILO_OK;
+}
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace milo

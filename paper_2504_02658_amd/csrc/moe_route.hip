@@ -11,7 +11,7 @@
 namespace milo {
 
 constexpr int kRouteMaxExperts = 1024, kRouteMaxTopk = 64;
-constexpr int kGateThreads = 256;
+constexpr int kGateThreads = 1024;
 
 struct GateArgs {
     const void* X;
@@ -86,27 +86,138 @@ __device__ __forceinline__ void choose_experts(const double* logits, int64_t t, 
     }
 }
 
+// Eight elements [k, k + 8) of a row of H, zeros beyond it.
+__device__ __forceinline__ u32x4 load8(const char* row, int64_t k, int64_t H) {
+    u32x4 r = {0u, 0u, 0u, 0u};
+    if (k + 8 <= H) {
+        __builtin_memcpy(&r, row + k * 2, 16);
+    } else {
+        const uint16_t* const p = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < H) r[i >> 1] |= (uint32_t)p[k + i] << (16 * (i & 1));
+    }
+    return r;
+}
 template <int IN>
-__global__ __launch_bounds__(kGateThreads) void moe_gate_kernel(const GateArgs a) {
+__device__ __forceinline__ double value8(const u32x4& r, int i) {
+    if constexpr (IN == W8_F16) return (double)(float)f16_bits((r[i >> 1] >> (16 * (i & 1))) & 0xffffu);
+    else return (double)__uint_as_float(i & 1 ? r[i >> 1] & 0xffff0000u : r[i >> 1] << 16);
+}
+
+// Few tokens: a workgroup per token, whose waves take four experts at a time, lanes along H.  Latency, and one compute unit's read of
+// the router's weight, bound it.
+template <int IN>
+__global__ __launch_bounds__(kGateThreads) void moe_gate_token_kernel(const GateArgs a) {
+    constexpr int G = 4;
     __shared__ double s_logit[kRouteMaxExperts];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t = blockIdx.x;
     const char* const x = reinterpret_cast<const char*>(a.X) + t * a.H * 2;
-    const int pieces = (int)((a.H + 15) / 16);
-    for (int e = wave; e < a.E; e += kGateThreads / 64) {
-        const char* const w = reinterpret_cast<const char*>(a.Wg) + e * a.H * 2;
-        double l = 0.0;
-        for (int p = lane; p < pieces; p += 64) {
-            const W8Raw<IN> xr = load16<IN>(x, (int64_t)p * 16, a.H), wr = load16<IN>(w, (int64_t)p * 16, a.H);
+    for (int e0 = wave * G; e0 < a.E; e0 += kGateThreads / 64 * G) {
+        const char* w[G];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) l = fma((double)raw_value<IN>(xr, i), (double)raw_value<IN>(wr, i), l);
+        for (int g = 0; g < G; ++g) w[g] = reinterpret_cast<const char*>(a.Wg) + (int64_t)(e0 + g < a.E ? e0 + g : a.E - 1) * a.H * 2;
+        double l[G] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 2
+        for (int64_t k = lane * 8; k < a.H; k += 512) {
+            const u32x4 xr = load8(x, k, a.H);
+            u32x4 wr[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) wr[g] = load8(w[g], k, a.H);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double v = value8<IN>(xr, i);
+#pragma unroll
+                for (int g = 0; g < G; ++g) l[g] = fma(v, value8<IN>(wr[g], i), l[g]);
+            }
         }
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
-        if (lane == 0) s_logit[e] = l;
+        for (int d = 32; d >= 1; d >>= 1)
+#pragma unroll
+            for (int g = 0; g < G; ++g) l[g] += __shfl_xor(l[g], d, 64);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (lane == 0 && e0 + g < a.E) s_logit[e0 + g] = l[g];
     }
     __syncthreads();
     if (wave == 0) choose_experts(s_logit, t, a);
+}
+
+// Many tokens: a workgroup takes 16 of them to all experts on the 64-bit matrix instructions, 64 experts at a time; its waves share H in
+// blocks of 32, of which lane (row, q) holds elements 8q .. 8q + 7 of its row, so that step j multiplies element j of every quarter.
+// The rate of those instructions bounds it (64 multiplications per cycle and compute unit).
+constexpr int kGateTileWaves = 8, kGateTileExperts = 256;
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+template <int IN>
+__global__ __launch_bounds__(kGateTileWaves * 64) void moe_gate_tile_kernel(const GateArgs a) {
+    __shared__ double s_logit[16][kGateTileExperts];
+    extern __shared__ __attribute__((aligned(32))) unsigned char smem[];
+    f64x4* const s_part = reinterpret_cast<f64x4*>(smem);           // [wave][tile][lane]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, q = lane >> 4;
+    const int64_t t0 = (int64_t)blockIdx.x * 16;
+    const int64_t row = t0 + r16 < a.T ? t0 + r16 : a.T - 1;
+    const char* const x = reinterpret_cast<const char*>(a.X) + row * a.H * 2;
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+        const char* w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = e0 + 16 * i + r16;
+            w[i] = reinterpret_cast<const char*>(a.Wg) + (int64_t)(e < a.E ? e : a.E - 1) * a.H * 2;
+        }
+        const int tiles = a.E - e0 >= 64 ? 4 : (a.E - e0 + 15) / 16;
+        f64x4 acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = f64x4{0.0, 0.0, 0.0, 0.0};
+        for (int64_t k0 = wave * 32; k0 < a.H; k0 += kGateTileWaves * 32) {
+            const u32x4 xr = load8(x, k0 + q * 8, a.H);
+            u32x4 wr[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < tiles) wr[i] = load8(w[i], k0 + q * 8, a.H);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const double v = value8<IN>(xr, j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < tiles) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(value8<IN>(wr[i], j), v, acc[i], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_part[(wave * 4 + i) * 64 + lane] = acc[i];
+        __syncthreads();
+        // lane (token r16, q) of tile i: experts 16 i + 4 j + q
+        for (int i = wave; i < tiles; i += kGateTileWaves) {
+            f64x4 s = s_part[i * 64 + lane];
+#pragma unroll
+            for (int v = 1; v < kGateTileWaves; ++v) s += s_part[(v * 4 + i) * 64 + lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int e = e0 + 16 * i + 4 * j + q;
+                if (e < a.E) s_logit[r16][e] = s[j];
+            }
+        }
+    }
+    __syncthreads();
+    for (int t = wave; t < 16; t += kGateTileWaves)
+        if (t0 + t < a.T) choose_experts(s_logit[t], t0 + t, a);
+}
+
+template <int IN>
+static int launch_gate(const GateArgs& a, hipStream_t stream) {
+    // From GATE_RULE
+    if (a.T > 1024 && a.E <= kGateTileExperts) {
+        constexpr int lds = kGateTileWaves * 4 * 64 * sizeof(f64x4);
+        static bool raised[64] = {false};
+        const int st = raise_lds(reinterpret_cast<const void*>(moe_gate_tile_kernel<IN>), lds, raised);
+        if (st != MILO_OK) return st;
+        moe_gate_tile_kernel<IN><<<dim3((unsigned)((a.T + 15) / 16)), dim3(kGateTileWaves * 64), lds, stream>>>(a);
+    } else {
+        moe_gate_token_kernel<IN><<<dim3((unsigned)a.T), dim3(kGateThreads), 0, stream>>>(a);
+    }
+    return launch_status();
 }
 
 }  // namespace milo
@@ -131,7 +242,5 @@ extern "C" int milo_moe_route(const milo_half* X, int64_t T, int64_t H, const mi
     a.renormalize = (flags & MILO_ROUTE_RENORMALIZE) != 0;
     a.ids = ids;
     a.gates = gates;
-    if (flags & MILO_ACT_BF16) moe_gate_kernel<W8_BF16><<<dim3((unsigned)T), dim3(kGateThreads), 0, (hipStream_t)stream>>>(a);
-    else moe_gate_kernel<W8_F16><<<dim3((unsigned)T), dim3(kGateThreads), 0, (hipStream_t)stream>>>(a);
-    return launch_status();
+    return flags & MILO_ACT_BF16 ? launch_gate<W8_BF16>(a, (hipStream_t)stream) : launch_gate<W8_F16>(a, (hipStream_t)stream);
 }

@@ -34,13 +34,32 @@ struct W8TileArgs {
     const void* w;                  // EPI 0
     const milo_w8_expert* experts;  // EPI 1, 2: device table
     const TileDesc* tiles;
-    int m_tiles, n_tiles;           // EPI 1, 2: m_tiles slots, some of them empty; the rest is set by launch_w8_tile
+    int m_tiles, n_tiles;           // EPI 1, 2: m_tiles slots, some of them empty; the rest is set at the launch
     const int32_t* x_rows;          // EPI 1: token of a sorted row;  EPI 2: pair of a sorted row
     const float* gates;             // EPI 2: factor per pair
     void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N] fp32
     int act_bf16;
 };
-int launch_w8_tile(const W8TileArgs& a, int epi, int bm, hipStream_t stream);
+// The kernels of a product, named by rows x features of a workgroup (EPI 1: half as many output features, from gate and up).
+enum W8Kernel { W8_WIDE_16x16, W8_WIDE_16x32, W8_WIDE_16x64, W8_WIDE_32x32, W8_WIDE_32x64, W8_WIDE_64x64, W8_TILE_64x128, W8_TILE_128x128, W8_TILE_128x256, W8_TILE_256x256 };
+int w8_kernel_rows(W8Kernel k);
+int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream);
+int launch_w8_wide(const W8TileArgs& a, int epi, int tm, int rn, hipStream_t stream);      // w8_wide.hip: 16 tm x 16 rn
+
+
+// Tile of a workgroup.  Workgroup i runs on XCD i % 8, each of which has an L2 of its own, so every XCD gets a contiguous range of
+// an order in which tiles that share rows or columns are close: groups of kW8GroupM tiles of rows, and inside a group all columns,
+// rows fastest.
+constexpr int kW8GroupM = 8;
+__device__ __forceinline__ void w8_tile_of(uint32_t i, int m_tiles, int n_tiles, int* mt, int* nt) {
+    const uint32_t total = (uint32_t)m_tiles * (uint32_t)n_tiles, x = i & 7u, per = total >> 3, rem = total & 7u;
+    const uint32_t l = x * per + (x < rem ? x : rem) + (i >> 3);
+    const uint32_t group = l / (uint32_t)(kW8GroupM * n_tiles), in = l - group * (uint32_t)(kW8GroupM * n_tiles);
+    const uint32_t left = (uint32_t)m_tiles - group * kW8GroupM, rows = left < kW8GroupM ? left : kW8GroupM;
+    *nt = (int)(in / rows);
+    *mt = (int)(group * kW8GroupM + in % rows);
+}
+
 
 bool w8_shape_ok(int64_t N, int64_t K);
 

@@ -1,4 +1,6 @@
 // Linears in 8-bit integers: milo_pack_w8, milo_w8a8_gemm and the tiled product that the MoE layer shares.
+#include <math.h>
+
 #include <type_traits>
 
 #include "milo_host.h"
@@ -16,13 +18,13 @@ bool w8_shape_ok(int64_t N, int64_t K) {
 // ---------------------------------------------------------------------------------------------
 // Row quantizer: a row is read once for its largest magnitude and, while it fits the registers of its TPR threads,
 // quantized from there.
-constexpr int kQuantThreads = 256, kQuantHeld = 4;
-template <int IN, int TPR, bool BLOCKED>
-__global__ __launch_bounds__(kQuantThreads) void w8_quant_kernel(const W8QuantArgs a, int kb) {
+constexpr int kQuantHeld = 4;
+template <int IN, int TPR, int ROWS, bool BLOCKED>
+__global__ __launch_bounds__(TPR * ROWS) void w8_quant_kernel(const W8QuantArgs a, int kb) {
     constexpr int SZ = IN == W8_F32 ? 4 : 2;
-    __shared__ uint32_t s_top[kQuantThreads / 64];
-    const int tid = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / TPR) + threadIdx.x / TPR;
+    __shared__ uint32_t s_top[TPR * ROWS / 64];
+    const int tid = threadIdx.x % TPR, of = threadIdx.x / TPR;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + of;
     const bool there = row < a.rows;
     const char* in = reinterpret_cast<const char*>(a.in) + (there ? row : 0) * a.K * SZ;
     const int64_t K = there ? a.K : 0;          // (rows beyond the last are all zero)
@@ -42,7 +44,10 @@ __global__ __launch_bounds__(kQuantThreads) void w8_quant_kernel(const W8QuantAr
         if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kQuantThreads / 64; ++w) top = s_top[w] > top ? s_top[w] : top;
+        for (int w = 0; w < TPR / 64; ++w) {
+            const uint32_t o = s_top[of * (TPR / 64) + w];
+            top = o > top ? o : top;
+        }
     }
     const RowStep st = row_step(top);
     if (!there && !BLOCKED) return;
@@ -66,10 +71,16 @@ static int launch_quant(const W8QuantArgs& a, hipStream_t stream) {
     const int kb = (int)w8_kblocks(a.K);
     const int64_t rows = BLOCKED ? w8_rblocks(a.rows) * 16 : a.rows;
     if (rows == 0) return MILO_OK;
-    if (kb * 4 <= 64 * kQuantHeld)      // a wave holds the whole row
-        w8_quant_kernel<IN, 64, BLOCKED><<<dim3((unsigned)((rows + 3) / 4)), dim3(kQuantThreads), 0, stream>>>(a, kb);
-    else
-        w8_quant_kernel<IN, 256, BLOCKED><<<dim3((unsigned)rows), dim3(kQuantThreads), 0, stream>>>(a, kb);
+    auto launch = [&](auto kernel, int threads, int per) { kernel<<<dim3((unsigned)((rows + per - 1) / per)), dim3(threads), 0, stream>>>(a, kb); };
+    const int pieces = kb * 4;
+    if (rows < 1024) {
+        if (pieces <= 256) launch(w8_quant_kernel<IN, 256, 1, BLOCKED>, 256, 1);
+        else launch(w8_quant_kernel<IN, 1024, 1, BLOCKED>, 1024, 1);
+    } else {
+        if (pieces <= 64 * kQuantHeld) launch(w8_quant_kernel<IN, 64, 16, BLOCKED>, 1024, 16);
+        else if (pieces <= 256 * kQuantHeld) launch(w8_quant_kernel<IN, 256, 4, BLOCKED>, 1024, 4);
+        else launch(w8_quant_kernel<IN, 1024, 1, BLOCKED>, 1024, 1);
+    }
     return launch_status();
 }
 int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream) {
@@ -83,66 +94,23 @@ int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream) {
     }
 }
 
-// ---------------------------------------------------------------------------------------------
-// Up to 16 rows: the weight's bytes bound the call.  A workgroup owns 16 output features, its waves share K chunk by
-// chunk (integer sums, so the split changes nothing), and each fragment of the weight goes from memory to the matrix
-// core's operand registers as it is.
-constexpr int kStreamWaves = 8;
-template <bool BF>
-__global__ __launch_bounds__(kStreamWaves * 64) void w8_stream_kernel(const uint8_t* __restrict__ xq, const float* __restrict__ xs, int64_t M, int64_t N, int64_t K,
-                                                                      const uint8_t* __restrict__ w, uint16_t* __restrict__ out) {
-    __shared__ i32x4 s_part[kStreamWaves][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kb = (int)w8_kblocks(K);
-    const u32x4* const wp = reinterpret_cast<const u32x4*>(w + (int64_t)blockIdx.x * kb * 1024) + lane;
-    const u32x4* const xp = reinterpret_cast<const u32x4*>(xq) + lane;
-    i32x4 acc = {0, 0, 0, 0};
-#pragma unroll 8
-    for (int b = wave; b < kb; b += kStreamWaves) acc = mfma16_i8(wp[(int64_t)b * 64], xp[(int64_t)b * 64], acc);
-    s_part[wave][lane] = acc;
-    __syncthreads();
-    if (wave != 0) return;
-#pragma unroll
-    for (int i = 1; i < kStreamWaves; ++i) acc += s_part[i][lane];
-    const int m = lane & 15;
-    const int64_t n = (int64_t)blockIdx.x * 16 + (lane >> 4) * 4;
-    if (m >= M || n >= N) return;
-    const float* sw = w8_scales(w, N, K) + n;
-    const float sx = xs[m];
-    float v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)acc[i] * sx * sw[i];
-    store4<BF>(out + m * N + n, v, (int)(N - n < 4 ? N - n : 4), (N & 3) == 0);
-}
-
-// ---------------------------------------------------------------------------------------------
-// Tile of a workgroup.  Workgroup i runs on XCD i % 8, each of which has an L2 of its own, so every XCD gets a contiguous range of
-// an order in which tiles that share rows or columns are close: groups of kGroupM tiles of rows, and inside a group all columns,
-// rows fastest.
-constexpr int kGroupM = 8;
-__device__ __forceinline__ void tile_of(uint32_t i, int m_tiles, int n_tiles, int* mt, int* nt) {
-    const uint32_t total = (uint32_t)m_tiles * (uint32_t)n_tiles, x = i & 7u, per = total >> 3, rem = total & 7u;
-    const uint32_t l = x * per + (x < rem ? x : rem) + (i >> 3);
-    const uint32_t group = l / (uint32_t)(kGroupM * n_tiles), in = l - group * (uint32_t)(kGroupM * n_tiles);
-    const uint32_t left = (uint32_t)m_tiles - group * kGroupM, rows = left < kGroupM ? left : kGroupM;
-    *nt = (int)(in / rows);
-    *mt = (int)(group * kGroupM + in % rows);
-}
-
 // The tiled product.
-template <int WM, int WN, int TM, int TN, int NS, int EPI, bool BF>
-__global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs a) {
+template <int WM, int WN, int WK, int TM, int TN, int NS, int EPI, bool BF>
+__global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8TileArgs a) {
     constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
-    constexpr int ABLK = BM / 16, BBLK = BN / 16;       // 1-KB blocks of a stage (64 columns)
+    constexpr int ABLK = BM / 16, BBLK = BN / 16;       // 1-KB blocks of 64 columns
     constexpr int PA = ABLK / NW, PB = BBLK / NW;       // of them, copied by one wave
-    constexpr int STAGE = (ABLK + BBLK) * 1024;
+    constexpr int PART = (ABLK + BBLK) * 1024, STAGE = WK * PART;
     constexpr int OUTN = EPI == 1 ? BN / 2 : BN;        // output columns of a tile
     static_assert(ABLK % NW == 0 && (EPI == 1 ? BBLK / 2 : BBLK) % NW == 0, "every wave copies as many blocks");
+    static_assert(WK == 1 || WK == 2, "an even number of blocks of 64 columns");
+    static_assert(WK == 1 || NS * STAGE >= NW * TM * TN * 4096, "room for the second half's sums");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kb = (int)w8_kblocks(a.K);
+    const int lane = threadIdx.x & 63, wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wk = wave_all / NW, wave = wave_all - wk * NW;
+    const int kb = (int)w8_kblocks(a.K), stages = kb / WK;
     int mt, nt;
-    tile_of(blockIdx.x, a.m_tiles, a.n_tiles, &mt, &nt);
+    w8_tile_of(blockIdx.x, a.m_tiles, a.n_tiles, &mt, &nt);
     const int64_t n0 = (int64_t)nt * OUTN;
     int64_t row0;
     int rows;
@@ -171,34 +139,37 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
     for (int i = 0; i < PA; ++i) {
         const int b = wave + i * NW;
         if constexpr (EPI == 0) {
-            aoff[i] = (uint32_t)(b * kb) * 1024u + lane * 16;
+            aoff[i] = (uint32_t)(b * kb + wk) * 1024u + lane * 16;
         } else {
             int r = b * 16 + (lane & 15);
             r = (int)row0 + (r < rows ? r : 0);         // (rows beyond the tile's: computed, not stored)
             const int64_t src = EPI == 1 ? a.x_rows[r] : r;
-            aoff[i] = (uint32_t)(src * kb * 64) + (lane >> 4) * 16;
+            aoff[i] = (uint32_t)(src * kb * 64) + wk * 64 + (lane >> 4) * 16;
         }
     }
 #pragma unroll
-    for (int i = 0; i < PB; ++i) boff[i] = (uint32_t)(((wave + i * NW) % (OUTN / 16)) * kb) * 1024u + lane * 16;
+    for (int i = 0; i < PB; ++i) boff[i] = (uint32_t)(((wave + i * NW) % (OUTN / 16)) * kb + wk) * 1024u + lane * 16;
     auto issue = [&](int c) {
-        unsigned char* const to = smem + (c % NS) * STAGE + wave * 1024;
+        unsigned char* const to = smem + (c % NS) * STAGE + wk * PART + wave * 1024;
 #pragma unroll
         for (int i = 0; i < PA; ++i) {
             const uint32_t o = aoff[i];
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsDst)(to + i * NW * 1024), 16, o, 0, 0, 0);
-            aoff[i] += EPI == 0 ? 1024u : 64u;
+            aoff[i] += (EPI == 0 ? 1024u : 64u) * WK;
         }
 #pragma unroll
         for (int i = 0; i < PB; ++i) {
             const uint32_t o = boff[i];
             if (EPI == 1 && i >= PB / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rb1, (LdsDst)(to + (ABLK + i * NW) * 1024), 16, o, 0, 0, 0);
             else __builtin_amdgcn_raw_ptr_buffer_load_lds(rb0, (LdsDst)(to + (ABLK + i * NW) * 1024), 16, o, 0, 0, 0);
-            boff[i] += 1024u;
+            boff[i] += 1024u * WK;
         }
     };
     const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, h = lane >> 5;
     const int frag = (l32 >> 4) * 1024 + h * 256 + (l32 & 15) * 16;
+    // The wave's m-th block of 32 rows is block m * WM + wm of the tile; blocks past the tile's rows take no part (the loop is there
+    // once for every number of blocks, and its body has no branches).
+    const int blocks = (rows + 31) / 32, used = (blocks - wm + WM - 1) / WM;
     i32x16 acc[TN][TM];
 #pragma unroll
     for (int n = 0; n < TN; ++n)
@@ -212,61 +183,99 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
     // way from LDS.  The copies of a wave complete in order: with at most those of the NS - 2 younger stages outstanding, stage
     // c + 1 is there; the barrier says so for all waves, and that all have read what they need of stage c, whose place the next
     // copies take.
-    u32x4 af[2][TM], bf[2][TN];
-    auto read = [&](int c, int k) {
-        const unsigned char* const as = smem + (c % NS) * STAGE + wm * TM * 2048 + frag + k * 512;
-        const unsigned char* const bs = smem + (c % NS) * STAGE + ABLK * 1024 + frag + k * 512;
+    auto k_loop = [&](auto mbu) {
+        constexpr int MBU = decltype(mbu)::value;
+        u32x4 af[2][MBU > 0 ? MBU : 1], bf[2][TN];
+        auto read = [&](int c, int k) {
+            const unsigned char* const as = smem + (c % NS) * STAGE + wk * PART + wm * 2048 + frag + k * 512;
+            const unsigned char* const bs = smem + (c % NS) * STAGE + wk * PART + ABLK * 1024 + frag + k * 512;
+            if constexpr (MBU > 0) {
 #pragma unroll
-        for (int n = 0; n < TN; ++n) bf[k][n] = *reinterpret_cast<const u32x4*>(bs + brow(n) * 2048);
+                for (int n = 0; n < TN; ++n) bf[k][n] = *reinterpret_cast<const u32x4*>(bs + brow(n) * 2048);
 #pragma unroll
-        for (int m = 0; m < TM; ++m) af[k][m] = *reinterpret_cast<const u32x4*>(as + m * 2048);
+                for (int m = 0; m < MBU; ++m) af[k][m] = *reinterpret_cast<const u32x4*>(as + m * WM * 2048);
+            }
+        };
+        auto multiply = [&](int k) {
+#pragma unroll
+            for (int m = 0; m < MBU; ++m)
+#pragma unroll
+                for (int n = 0; n < TN; ++n) acc[n][m] = mfma32_i8(bf[k][n], af[k][m], acc[n][m]);
+        };
+        // one LDS read behind each of the first matrix instructions, instead of all of them in front
+        auto mix = [&] {
+            if constexpr (MBU * TN >= MBU + TN) {
+#pragma unroll
+                for (int i = 0; i < MBU + TN; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x8, MBU * TN - MBU - TN, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto arrive = [&](auto counted, bool all) {
+            if (!decltype(counted)::value && all) wait_vmem();
+            else MILO_WAIT_VMEM((NS - 2) * (PA + PB));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        for (int c = 0; c < NS - 1 && c < stages; ++c) issue(c);
+        arrive(std::bool_constant<false>{}, stages < NS - 1);
+        if (NS - 1 < stages) issue(NS - 1);
+        read(0, 0);
+        int c = 0;
+        auto stage = [&](auto more) {           // more: stage c + NS exists
+            read(c, 1);
+            multiply(0);
+            mix();
+            arrive(more, true);
+            if constexpr (decltype(more)::value) issue(c + NS);
+            read(c + 1, 0);                     // (behind the last stage: of no use)
+            multiply(1);
+            mix();
+        };
+        for (; c + NS < stages; ++c) stage(std::bool_constant<true>{});
+        for (; c < stages; ++c) stage(std::bool_constant<false>{});
     };
-    auto multiply = [&](int k) {
-#pragma unroll
-        for (int m = 0; m < TM; ++m)
-#pragma unroll
-            for (int n = 0; n < TN; ++n) acc[n][m] = mfma32_i8(bf[k][n], af[k][m], acc[n][m]);
-    };
-    // one LDS read behind each of the first matrix instructions, instead of all of them in front
-    auto mix = [&] {
-#pragma unroll
-        for (int i = 0; i < TM + TN; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x8, TM * TN - TM - TN, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto arrive = [&](auto counted, bool all) {
-        if (!decltype(counted)::value && all) wait_vmem();
-        else MILO_WAIT_VMEM((NS - 2) * (PA + PB));
+    if (TM >= 4 && used >= 4) k_loop(std::integral_constant<int, TM >= 4 ? 4 : 1>{});
+    else if (TM >= 3 && used == 3) k_loop(std::integral_constant<int, TM >= 3 ? 3 : 1>{});
+    else if (TM >= 2 && used >= 2) k_loop(std::integral_constant<int, TM >= 2 ? 2 : 1>{});
+    else if (used >= 1) k_loop(std::integral_constant<int, 1>{});
+    else k_loop(std::integral_constant<int, 0>{});          // (copies its share, and keeps the barriers)
+    if constexpr (WK == 2) {
+        // the waves of the odd blocks hand their sums to those of the even ones, through the stages that nobody reads any more
+        i32x4* const part = reinterpret_cast<i32x4*>(smem) + wave * (TM * TN * 256) + lane;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
-    for (int c = 0; c < NS - 1 && c < kb; ++c) issue(c);
-    arrive(std::bool_constant<false>{}, kb < NS - 1);
-    if (NS - 1 < kb) issue(NS - 1);
-    read(0, 0);
-    int c = 0;
-    auto stage = [&](auto more) {           // more: stage c + NS exists
-        read(c, 1);
-        multiply(0);
-        mix();
-        arrive(more, true);
-        if constexpr (decltype(more)::value) issue(c + NS);
-        read(c + 1, 0);                     // (behind the last stage: of no use)
-        multiply(1);
-        mix();
-    };
-    for (; c + NS < kb; ++c) stage(std::bool_constant<true>{});
-    for (; c < kb; ++c) stage(std::bool_constant<false>{});
+        __syncthreads();
+        if (wk == 1) {
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) part[((n * TM + m) * 4 + i) * 64] = i32x4{acc[n][m][4 * i], acc[n][m][4 * i + 1], acc[n][m][4 * i + 2], acc[n][m][4 * i + 3]};
+        }
+        __syncthreads();
+        if (wk == 1) return;
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const i32x4 v = part[((n * TM + m) * 4 + i) * 64];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[n][m][4 * i + j] += v[j];
+                }
+    }
     // lane: row (of 32) l32, output features 8 i + 4 h + 0..3
     const bool vec = (a.N & 3) == 0;
     const auto sw0 = global_float(w8_scales(w0, a.N, a.K)), sw1 = global_float(w8_scales(w1, a.N, a.K));
 #pragma unroll
     for (int m = 0; m < TM; ++m) {
-        const int r = (wm * TM + m) * 32 + l32;
+        const int r = (m * WM + wm) * 32 + l32;
         if (r >= rows) continue;
         const int64_t row = row0 + r;
         float sx;
@@ -302,33 +311,88 @@ __global__ __launch_bounds__(WM * WN * 64) void w8_tile_kernel(const W8TileArgs 
     }
 }
 
-template <int WM, int WN, int TM, int TN, int NS, int EPI, bool BF>
+template <int WM, int WN, int WK, int TM, int TN, int NS, int EPI, bool BF>
 static int launch_tile(W8TileArgs a, hipStream_t stream) {
-    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, OUTN = EPI == 1 ? BN / 2 : BN, lds = NS * (BM + BN) * 64;
+    constexpr int BM = WM * TM * 32, BN = WN * TN * 32, OUTN = EPI == 1 ? BN / 2 : BN, lds = NS * WK * (BM + BN) * 64;
     if constexpr (lds > 64 * 1024) {
         static bool raised[64] = {false};
-        int dev = 0;
-        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MILO_ERR_HIP;
-        if (!raised[dev]) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_tile_kernel<WM, WN, TM, TN, NS, EPI, BF>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-                return MILO_ERR_HIP;
-            raised[dev] = true;
-        }
+        const int st = raise_lds(reinterpret_cast<const void*>(w8_tile_kernel<WM, WN, WK, TM, TN, NS, EPI, BF>), lds, raised);
+        if (st != MILO_OK) return st;
     }
     if (EPI == 0) a.m_tiles = (int)((a.M + BM - 1) / BM);
     a.n_tiles = (int)((a.N + OUTN - 1) / OUTN);
-    if ((int64_t)a.m_tiles * a.n_tiles > (int64_t(1) << 31) / (WM * WN * 64)) return MILO_ERR_SHAPE;
-    w8_tile_kernel<WM, WN, TM, TN, NS, EPI, BF><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(WM * WN * 64), lds, stream>>>(a);
+    if ((int64_t)a.m_tiles * a.n_tiles > (int64_t(1) << 31) / (WM * WN * WK * 64)) return MILO_ERR_SHAPE;
+    w8_tile_kernel<WM, WN, WK, TM, TN, NS, EPI, BF><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(WM * WN * WK * 64), lds, stream>>>(a);
     return launch_status();
 }
 template <int EPI, bool BF>
-static int launch_tile_bm(const W8TileArgs& a, int bm, hipStream_t stream) {
-    if (bm == 256) return launch_tile<2, 4, 4, 2, 4, EPI, BF>(a, stream);
-    return launch_tile<2, 2, 2, 2, 4, EPI, BF>(a, stream);
+static int launch_tile_shape(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
+    switch (k) {
+        case W8_TILE_64x128: return launch_tile<2, 2, 2, 1, 2, 4, EPI, BF>(a, stream);
+        case W8_TILE_128x128: return launch_tile<2, 2, 1, 2, 2, 4, EPI, BF>(a, stream);
+        case W8_TILE_128x256: return launch_tile<2, 4, 1, 2, 2, 6, EPI, BF>(a, stream);
+        default: return launch_tile<2, 4, 1, 4, 2, 4, EPI, BF>(a, stream);
+    }
 }
-int launch_w8_tile(const W8TileArgs& a, int epi, int bm, hipStream_t stream) {
-    if (epi == 0) return a.act_bf16 ? launch_tile_bm<0, true>(a, bm, stream) : launch_tile_bm<0, false>(a, bm, stream);
-    return epi == 1 ? launch_tile_bm<1, false>(a, bm, stream) : launch_tile_bm<2, false>(a, bm, stream);
+static int launch_w8_tile(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream) {
+    if (epi == 0) return a.act_bf16 ? launch_tile_shape<0, true>(a, k, stream) : launch_tile_shape<0, false>(a, k, stream);
+    return epi == 1 ? launch_tile_shape<1, false>(a, k, stream) : launch_tile_shape<2, false>(a, k, stream);
+}
+int w8_kernel_rows(W8Kernel k) {
+    switch (k) {
+        case W8_WIDE_16x16: case W8_WIDE_16x32: case W8_WIDE_16x64: return 16;
+        case W8_WIDE_32x32: case W8_WIDE_32x64: return 32;
+        case W8_WIDE_64x64: case W8_TILE_64x128: return 64;
+        case W8_TILE_128x128: case W8_TILE_128x256: return 128;
+        default: return 256;
+    }
+}
+int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream) {
+    switch (k) {
+        case W8_WIDE_16x16: return launch_w8_wide(a, epi, 1, 1, stream);
+        case W8_WIDE_16x32: return launch_w8_wide(a, epi, 1, 2, stream);
+        case W8_WIDE_16x64: return launch_w8_wide(a, epi, 1, 4, stream);
+        case W8_WIDE_32x32: return launch_w8_wide(a, epi, 2, 2, stream);
+        case W8_WIDE_32x64: return launch_w8_wide(a, epi, 2, 4, stream);
+        case W8_WIDE_64x64: return launch_w8_wide(a, epi, 4, 4, stream);
+        default: return launch_w8_tile(a, epi, k, stream);
+    }
+}
+
+// The kernel of a linear.  Up to 16 rows every weight byte is read once, and what counts is that all compute units read: as many features
+// per workgroup as leave at least 192 workgroups (16 rows, N = 14336, K = 4096: 20.4, 18.8, 18.2 us with 16, 32, 64 features; N = 4096,
+// K = 14336: 20.3, 24.2, 31.4).  More rows: the least of the estimates
+//     base + blocks of 64 columns * (lat + step * max(rounds, full * workgroups per compute unit))
+// with rounds = 1 for the kernels whose workgroups share a compute unit, else the workgroups per compute unit rounded up, and the constants
+// (us, at 256 compute units) fitted to 2520 times of 180 shapes, 1 to 4096 rows, N and K from 512 to 14336, in every kernel.  The
+// choice costs 3.5 % against the best of 14 kernels of each shape on average, 25 % at worst (96 x 8192 x 8192); 32 x 64 or 256 x 256,
+// whichever is better, would cost 13 %.
+W8Kernel w8_linear_kernel(int64_t M, int64_t N, int64_t K) {
+    if (M <= 16) return N >= 192 * 64 ? W8_WIDE_16x64 : N >= 192 * 32 ? W8_WIDE_16x32 : W8_WIDE_16x16;
+    struct Cost {
+        W8Kernel kernel;
+        int rows, cols;
+        bool whole;         // whole rounds
+        double base, lat, step, full;
+    };
+    static const Cost costs[] = {
+        {W8_WIDE_16x32, 16, 32, false, 7.91, 0.0235, 0.0118, 3.56}, {W8_WIDE_32x32, 32, 32, false, 8.16, 0.0243, 0.0378, 1.60},
+        {W8_WIDE_32x64, 32, 64, false, 8.71, 0.0474, 0.0056, 13.9}, {W8_WIDE_64x64, 64, 64, false, 9.51, 0.0158, 0.0882, 1.64},
+        {W8_TILE_64x128, 64, 128, true, 8.76, 0.0, 0.240, 1.24},    {W8_TILE_128x128, 128, 128, true, 13.7, 0.0218, 0.235, 1.26},
+        {W8_TILE_128x256, 128, 256, true, 12.7, 0.0, 0.456, 1.25},  {W8_TILE_256x256, 256, 256, true, 14.5, 0.0, 0.759, 1.26}};
+    W8Kernel best = W8_TILE_256x256;
+    double least = 0.0;
+    const double kb = (double)w8_kblocks(K), cus = device_cus();
+    for (const Cost& c : costs) {
+        const double groups = (double)((M + c.rows - 1) / c.rows) * (double)((N + c.cols - 1) / c.cols) / cus;
+        const double per = fmax(c.whole ? ceil(groups) : 1.0, c.full * groups);
+        const double t = c.base + kb * (c.lat + c.step * per);
+        if (least == 0.0 || t < least) {
+            least = t;
+            best = c.kernel;
+        }
+    }
+    return best;
 }
 
 }  // namespace milo
@@ -377,12 +441,6 @@ extern "C" int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t 
     q.blocked = 1;
     int st = launch_w8_quant(q, bf ? W8_BF16 : W8_F16, (hipStream_t)stream);
     if (st != MILO_OK) return st;
-    if (M <= 16) {
-        const dim3 grid((unsigned)w8_rblocks(N)), block(kStreamWaves * 64);
-        if (bf) w8_stream_kernel<true><<<grid, block, 0, (hipStream_t)stream>>>(q.codes, q.scales, M, N, K, (const uint8_t*)w8, Y);
-        else w8_stream_kernel<false><<<grid, block, 0, (hipStream_t)stream>>>(q.codes, q.scales, M, N, K, (const uint8_t*)w8, Y);
-        return launch_status();
-    }
     W8TileArgs a = {};
     a.A = q.codes;
     a.a_bytes = (uint64_t)w8_code_bytes(M, K);
@@ -393,5 +451,8 @@ extern "C" int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t 
     a.w = w8;
     a.out = Y;
     a.act_bf16 = bf;
-    return launch_w8_tile(a, 0, M > 128 ? 256 : 128, (hipStream_t)stream);
+    return launch_w8_product(a, 0, w8_linear_kernel(M, N, K), (hipStream_t)stream);
 }
+
+// For the tests: which kernel a linear takes (W8Kernel; for the current device, or without one for 256 compute units).
+extern "C" int milo_w8a8_route(int64_t M, int64_t N, int64_t K) { return (int)w8_linear_kernel(M, N, K); }

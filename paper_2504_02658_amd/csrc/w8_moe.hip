@@ -337,13 +337,8 @@ template <bool BF, bool STAGED>
 static int launch_few_down(const W8FewArgs& a, dim3 grid, int lds, hipStream_t stream) {
     if constexpr (STAGED) {
         static bool raised[64] = {false};
-        int dev = 0;
-        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MILO_ERR_HIP;
-        if (!raised[dev]) {
-            if (hipFuncSetAttribute(reinterpret_cast<const void*>(w8_few_down_kernel<BF, STAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kFewDownStaged) != hipSuccess)
-                return MILO_ERR_HIP;
-            raised[dev] = true;
-        }
+        const int st = raise_lds(reinterpret_cast<const void*>(w8_few_down_kernel<BF, STAGED>), kFewDownStaged, raised);
+        if (st != MILO_OK) return st;
     }
     w8_few_down_kernel<BF, STAGED><<<grid, dim3(kFewDownThreads), lds, stream>>>(a);
     return launch_status();
@@ -405,6 +400,7 @@ __global__ __launch_bounds__(256) void w8_combine_kernel(const float* __restrict
 // Workspace of a forward.
 struct W8MoeLayout {
     bool few;
+    W8Kernel kernel;
     int bm, max_tiles;
     size_t off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
 };
@@ -431,7 +427,12 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         L->off_hq = take((size_t)(P * fb));
         L->off_hs = take((size_t)P * 4);
     } else {
-        L->bm = P >= 192 * (int64_t)E ? 256 : 128;
+        // Rows per expert decide: the weights' bytes bound a few of them, and a tile of 32 x 64 has them on their way soonest (66 experts of
+        // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256); from a hundred on the matrix cores do (8 experts of
+        // 14336 x 4096, 512 tokens: 513 us with tiles of 256 x 256 against 520 and 626 with 128 x 256 and 128 x 128; 64 tokens: 307, 300, 311).
+        const int64_t met = P < E ? P : E, per = P / met;
+        L->kernel = per < 12 ? W8_WIDE_32x64 : per < 96 ? W8_TILE_128x256 : W8_TILE_256x256;
+        L->bm = w8_kernel_rows(L->kernel);
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
         L->off_sorted = take((size_t)P * 4);
         L->off_token = take((size_t)P * 4);
@@ -530,7 +531,7 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.m_tiles = L.max_tiles;
     t.x_rows = g.sorted_token;
     t.out = ws + L.off_h;
-    st = launch_w8_tile(t, 1, L.bm, s);
+    st = launch_w8_product(t, 1, L.kernel, s);
     if (st != MILO_OK) return st;
     q.in = ws + L.off_h;
     q.rows = P;
@@ -547,7 +548,7 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.x_rows = g.sorted;
     t.gates = topk_weights;
     t.out = ws + L.off_o;
-    st = launch_w8_tile(t, 2, L.bm, s);
+    st = launch_w8_product(t, 2, L.kernel, s);
     if (st != MILO_OK) return st;
     const float* const O = reinterpret_cast<const float*>(ws + L.off_o);
     if (bf) w8_combine_kernel<true><<<dim3((unsigned)T), dim3(256), 0, s>>>(O, topk_ids, topk, E, H, Y);
