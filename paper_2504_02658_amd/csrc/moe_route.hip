@@ -29,38 +29,67 @@ __device__ __forceinline__ int64_t logit_key(double l) {
     return b < 0 ? (b ^ INT64_MAX) : b;
 }
 
+// Largest value of a wave, by rows of 16 and then across them, in every lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t max_step(int64_t v) {
+    const int lo = (int)(uint32_t)v, hi = (int)(v >> 32);
+    const uint32_t olo = (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, CTRL, ROWS, 0xf, false);
+    const int ohi = __builtin_amdgcn_update_dpp(hi, hi, CTRL, ROWS, 0xf, false);
+    const int64_t o = (int64_t)ohi << 32 | olo;
+    return o > v ? o : v;
+}
+__device__ __forceinline__ int64_t wave_max_key(int64_t v) {
+    v = max_step<0x111, 0xf>(v);        // row_shr 1, 2, 4, 8: lane 15 of a row has the row's
+    v = max_step<0x112, 0xf>(v);
+    v = max_step<0x114, 0xf>(v);
+    v = max_step<0x118, 0xf>(v);
+    v = max_step<0x142, 0xa>(v);        // row_bcast 15 and 31: lane 63 has the wave's
+    v = max_step<0x143, 0xc>(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+    const int hi = __builtin_amdgcn_readlane((int)(v >> 32), 63);
+    return (int64_t)hi << 32 | lo;
+}
+
 // One wave chooses from logits[0, E) of one token and writes the token's row of ids and gates.
 __device__ __forceinline__ void choose_experts(const double* logits, int64_t t, const GateArgs& a) {
     const int lane = threadIdx.x & 63, width = a.topk + a.n_shared;
     uint32_t taken = 0u;        // of expert lane + 64 i: bit i
     int my_id = 0;
     double top = 0.0, my_logit = 0.0;
-    for (int j = 0; j < a.topk; ++j) {
-        int64_t key = INT64_MIN;
-        int id = 0x7fffffff;
+    int64_t key = INT64_MIN;    // of this lane's best expert that is left, and the expert (-1: none)
+    int id = -1;
+    auto best_left = [&] {
+        key = INT64_MIN;
+        id = -1;
         for (int i = 0, e = lane; e < a.E; ++i, e += 64)
             if (!(taken >> i & 1)) {
                 const int64_t k = logit_key(logits[e]);
-                if (k > key || id == 0x7fffffff) {
+                if (k > key || id < 0) {
                     key = k;
                     id = e;
                 }
             }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) {
-            const int64_t ok = __shfl_xor((long long)key, d, 64);
-            const int oi = __shfl_xor(id, d, 64);
-            if (oi != 0x7fffffff && (id == 0x7fffffff || ok > key || (ok == key && oi < id))) {
-                key = ok;
-                id = oi;
-            }
+    };
+    best_left();
+    for (int j = 0; j < a.topk; ++j) {
+        const int64_t most = wave_max_key(key);
+        // (topk <= E: some lane has it; of equal ones the lowest id)
+        unsigned long long m = __builtin_amdgcn_ballot_w64(id >= 0 && key == most);
+        int first = 0x7fffffff;
+        while (m) {
+            const int e = __builtin_amdgcn_readlane(id, (int)__builtin_ctzll(m));
+            first = e < first ? e : first;
+            m &= m - 1;
         }
-        if ((id & 63) == lane) taken |= 1u << (id >> 6);
-        const double l = logits[id];
+        const double l = logits[first];
         if (j == 0) top = l;
         if (lane == j) {
-            my_id = id;
+            my_id = first;
             my_logit = l;
+        }
+        if ((first & 63) == lane) {
+            taken |= 1u << (first >> 6);
+            best_left();
         }
     }
     // (a NaN logit, infinite ones or a NaN in the inputs: every gate of the token is NaN, as the quotient gives)
@@ -144,12 +173,12 @@ __global__ __launch_bounds__(kGateThreads) void moe_gate_token_kernel(const Gate
     if (wave == 0) choose_experts(s_logit, t, a);
 }
 
-// Many tokens: a workgroup takes 16 of them to all experts on the 64-bit matrix instructions, 64 experts at a time; its waves share H in
+// Many tokens: a workgroup takes 16 of them to all experts on the 64-bit matrix instructions, 16 TILES experts at a time; its waves share H in
 // blocks of 32, of which lane (row, q) holds elements 8q .. 8q + 7 of its row, so that step j multiplies element j of every quarter.
 // The rate of those instructions bounds it (64 multiplications per cycle and compute unit).
 constexpr int kGateTileWaves = 8, kGateTileExperts = 256;
 typedef double f64x4 __attribute__((ext_vector_type(4)));
-template <int IN>
+template <int IN, int TILES>
 __global__ __launch_bounds__(kGateTileWaves * 64) void moe_gate_tile_kernel(const GateArgs a) {
     __shared__ double s_logit[16][kGateTileExperts];
     extern __shared__ __attribute__((aligned(32))) unsigned char smem[];
@@ -159,40 +188,48 @@ __global__ __launch_bounds__(kGateTileWaves * 64) void moe_gate_tile_kernel(cons
     const int64_t t0 = (int64_t)blockIdx.x * 16;
     const int64_t row = t0 + r16 < a.T ? t0 + r16 : a.T - 1;
     const char* const x = reinterpret_cast<const char*>(a.X) + row * a.H * 2;
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
-        const char* w[4];
+    for (int e0 = 0; e0 < a.E; e0 += 16 * TILES) {
+        const char* w[TILES];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < TILES; ++i) {
             const int e = e0 + 16 * i + r16;
             w[i] = reinterpret_cast<const char*>(a.Wg) + (int64_t)(e < a.E ? e : a.E - 1) * a.H * 2;
         }
-        const int tiles = a.E - e0 >= 64 ? 4 : (a.E - e0 + 15) / 16;
-        f64x4 acc[4];
+        f64x4 acc[TILES];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = f64x4{0.0, 0.0, 0.0, 0.0};
-        for (int64_t k0 = wave * 32; k0 < a.H; k0 += kGateTileWaves * 32) {
-            const u32x4 xr = load8(x, k0 + q * 8, a.H);
-            u32x4 wr[4];
+        for (int i = 0; i < TILES; ++i) acc[i] = f64x4{0.0, 0.0, 0.0, 0.0};
+        u32x4 xr[2], wr[2][TILES];
+        auto fetch = [&](int64_t k, int to) {
+            xr[to] = load8(x, k + q * 8, a.H);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < tiles) wr[i] = load8(w[i], k0 + q * 8, a.H);
+            for (int i = 0; i < TILES; ++i) wr[to][i] = load8(w[i], k + q * 8, a.H);
+        };
+        auto work = [&](int64_t k, int from) {
+            fetch(k + kGateTileWaves * 32, from ^ 1);
+            asm volatile("" ::: "memory");              // (the loads stay in front)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const double v = value8<IN>(xr, j);
+                const double v = value8<IN>(xr[from], j);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < tiles) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(value8<IN>(wr[i], j), v, acc[i], 0, 0, 0);
+                for (int i = 0; i < TILES; ++i) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(value8<IN>(wr[from][i], j), v, acc[i], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        fetch(wave * 32, 0);
+        for (int64_t k = wave * 32; k < a.H; k += 2 * kGateTileWaves * 32) {
+            work(k, 0);
+            if (k + kGateTileWaves * 32 >= a.H) break;
+            work(k + kGateTileWaves * 32, 1);
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s_part[(wave * 4 + i) * 64 + lane] = acc[i];
+        for (int i = 0; i < TILES; ++i) s_part[(wave * TILES + i) * 64 + lane] = acc[i];
         __syncthreads();
         // lane (token r16, q) of tile i: experts 16 i + 4 j + q
-        for (int i = wave; i < tiles; i += kGateTileWaves) {
+        for (int i = wave; i < TILES; i += kGateTileWaves) {
             f64x4 s = s_part[i * 64 + lane];
 #pragma unroll
-            for (int v = 1; v < kGateTileWaves; ++v) s += s_part[(v * 4 + i) * 64 + lane];
+            for (int v = 1; v < kGateTileWaves; ++v) s += s_part[(v * TILES + i) * 64 + lane];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int e = e0 + 16 * i + 4 * j + q;
@@ -205,18 +242,19 @@ __global__ __launch_bounds__(kGateTileWaves * 64) void moe_gate_tile_kernel(cons
         if (t0 + t < a.T) choose_experts(s_logit[t], t0 + t, a);
 }
 
+template <int IN, int TILES>
+static int launch_gate_tile(const GateArgs& a, hipStream_t stream) {
+    constexpr int lds = kGateTileWaves * TILES * 64 * sizeof(f64x4);
+    static bool raised[64] = {false};
+    const int st = raise_lds(reinterpret_cast<const void*>(moe_gate_tile_kernel<IN, TILES>), lds, raised);
+    if (st != MILO_OK) return st;
+    moe_gate_tile_kernel<IN, TILES><<<dim3((unsigned)((a.T + 15) / 16)), dim3(kGateTileWaves * 64), lds, stream>>>(a);
+    return launch_status();
+}
 template <int IN>
 static int launch_gate(const GateArgs& a, hipStream_t stream) {
-    // From GATE_RULE
-    if (a.T > 1024 && a.E <= kGateTileExperts) {
-        constexpr int lds = kGateTileWaves * 4 * 64 * sizeof(f64x4);
-        static bool raised[64] = {false};
-        const int st = raise_lds(reinterpret_cast<const void*>(moe_gate_tile_kernel<IN>), lds, raised);
-        if (st != MILO_OK) return st;
-        moe_gate_tile_kernel<IN><<<dim3((unsigned)((a.T + 15) / 16)), dim3(kGateTileWaves * 64), lds, stream>>>(a);
-    } else {
-        moe_gate_token_kernel<IN><<<dim3((unsigned)a.T), dim3(kGateThreads), 0, stream>>>(a);
-    }
+    if (a.T > 1024 && a.E <= kGateTileExperts) return a.E <= 16 ? launch_gate_tile<IN, 1>(a, stream) : launch_gate_tile<IN, 4>(a, stream);
+    moe_gate_token_kernel<IN><<<dim3((unsigned)a.T), dim3(kGateThreads), 0, stream>>>(a);
     return launch_status();
 }
 
