@@ -41,7 +41,7 @@ struct W8TileArgs {
     int act_bf16;
 };
 // The kernels of a product, named by rows x features of a workgroup (EPI 1: half as many output features, from gate and up).
-enum W8Kernel { W8_WIDE_16x16, W8_WIDE_16x32, W8_WIDE_16x64, W8_WIDE_32x32, W8_WIDE_32x64, W8_WIDE_64x64, W8_TILE_64x128, W8_TILE_128x128, W8_TILE_128x256, W8_TILE_256x256 };
+enum W8Kernel { W8_WIDE_16x16, W8_WIDE_16x32, W8_WIDE_16x64, W8_WIDE_32x32, W8_WIDE_32x64, W8_WIDE_64x64, W8_TILE_64x128, W8_TILE_128x128, W8_TILE_128x256 };
 int w8_kernel_rows(W8Kernel k);
 int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream);
 int launch_w8_wide(const W8TileArgs& a, int epi, int tm, int rn, hipStream_t stream);      // w8_wide.hip: 16 tm x 16 rn

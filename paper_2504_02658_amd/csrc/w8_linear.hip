@@ -330,8 +330,7 @@ static int launch_tile_shape(const W8TileArgs& a, W8Kernel k, hipStream_t stream
     switch (k) {
         case W8_TILE_64x128: return launch_tile<2, 2, 2, 1, 2, 4, EPI, BF>(a, stream);
         case W8_TILE_128x128: return launch_tile<2, 2, 1, 2, 2, 4, EPI, BF>(a, stream);
-        case W8_TILE_128x256: return launch_tile<2, 4, 1, 2, 2, 6, EPI, BF>(a, stream);
-        default: return launch_tile<2, 4, 1, 4, 2, 4, EPI, BF>(a, stream);
+        default: return launch_tile<2, 4, 1, 2, 2, 3, EPI, BF>(a, stream);      // (72 KB of LDS: two workgroups share a compute unit)
     }
 }
 static int launch_w8_tile(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream) {
@@ -343,8 +342,7 @@ int w8_kernel_rows(W8Kernel k) {
         case W8_WIDE_16x16: case W8_WIDE_16x32: case W8_WIDE_16x64: return 16;
         case W8_WIDE_32x32: case W8_WIDE_32x64: return 32;
         case W8_WIDE_64x64: case W8_TILE_64x128: return 64;
-        case W8_TILE_128x128: case W8_TILE_128x256: return 128;
-        default: return 256;
+        default: return 128;
     }
 }
 int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream) {
@@ -366,7 +364,8 @@ int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stre
 // with rounds = 1 for the kernels whose workgroups share a compute unit, else the workgroups per compute unit rounded up, and the constants
 // (us, at 256 compute units) fitted to 2520 times of 180 shapes, 1 to 4096 rows, N and K from 512 to 14336, in every kernel.  The
 // choice costs 3.5 % against the best of 14 kernels of each shape on average, 25 % at worst (96 x 8192 x 8192); 32 x 64 or 256 x 256,
-// whichever is better, would cost 13 %.
+// whichever is better, would cost 13 %.  (Tiles of 256 x 256 are gone: with their 128 KB of LDS a compute unit has one workgroup and nothing to do
+// in its epilogue; 4096 x 2048 x 1408 41.4 us against 33.7, 4096 x 14336 x 4096 298 against 296, 4096 x 4096 x 14336 257 against 265.)
 W8Kernel w8_linear_kernel(int64_t M, int64_t N, int64_t K) {
     if (M <= 16) return N >= 192 * 64 ? W8_WIDE_16x64 : N >= 192 * 32 ? W8_WIDE_16x32 : W8_WIDE_16x16;
     struct Cost {
@@ -379,8 +378,8 @@ W8Kernel w8_linear_kernel(int64_t M, int64_t N, int64_t K) {
         {W8_WIDE_16x32, 16, 32, false, 7.91, 0.0235, 0.0118, 3.56}, {W8_WIDE_32x32, 32, 32, false, 8.16, 0.0243, 0.0378, 1.60},
         {W8_WIDE_32x64, 32, 64, false, 8.71, 0.0474, 0.0056, 13.9}, {W8_WIDE_64x64, 64, 64, false, 9.51, 0.0158, 0.0882, 1.64},
         {W8_TILE_64x128, 64, 128, true, 8.76, 0.0, 0.240, 1.24},    {W8_TILE_128x128, 128, 128, true, 13.7, 0.0218, 0.235, 1.26},
-        {W8_TILE_128x256, 128, 256, true, 12.7, 0.0, 0.456, 1.25},  {W8_TILE_256x256, 256, 256, true, 14.5, 0.0, 0.759, 1.26}};
-    W8Kernel best = W8_TILE_256x256;
+        {W8_TILE_128x256, 128, 256, true, 12.7, 0.0, 0.456, 1.25}};
+    W8Kernel best = W8_TILE_128x256;
     double least = 0.0;
     const double kb = (double)w8_kblocks(K), cus = device_cus();
     for (const Cost& c : costs) {

@@ -427,11 +427,10 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         L->off_hq = take((size_t)(P * fb));
         L->off_hs = take((size_t)P * 4);
     } else {
-        // Rows per expert decide: the weights' bytes bound a few of them, and a tile of 32 x 64 has them on their way soonest (66 experts of
-        // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256); from a hundred on the matrix cores do (8 experts of
-        // 14336 x 4096, 512 tokens: 513 us with tiles of 256 x 256 against 520 and 626 with 128 x 256 and 128 x 128; 64 tokens: 307, 300, 311).
-        const int64_t met = P < E ? P : E, per = P / met;
-        L->kernel = per < 12 ? W8_WIDE_32x64 : per < 96 ? W8_TILE_128x256 : W8_TILE_256x256;
+        // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest (66 experts of
+        // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256; 8 experts of 14336 x 4096, 64 tokens: 331 against 300).
+        const int64_t met = P < E ? P : E;
+        L->kernel = P < 12 * met ? W8_WIDE_32x64 : W8_TILE_128x256;
         L->bm = w8_kernel_rows(L->kernel);
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
         L->off_sorted = take((size_t)P * 4);
