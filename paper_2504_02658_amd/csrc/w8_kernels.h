@@ -22,6 +22,9 @@ struct W8QuantArgs {
 };
 int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream);
 
+constexpr int kW8HBlock = 128;
+int launch_w8_requant(const int16_t* in, const float* block_scales, int64_t rows, int64_t K, uint8_t* codes, float* scales, hipStream_t stream);
+
 // Tiled product.  Row r of a tile's A operand:
 //   EPI 0 (a linear):         blocked activations, row 'tile * BM + r' of M
 //   EPI 1 (gate and up):      row-major activations, row x_rows[row0 + r]
@@ -37,7 +40,11 @@ struct W8TileArgs {
     int m_tiles, n_tiles;           // EPI 1, 2: m_tiles slots, some of them empty; the rest is set at the launch
     const int32_t* x_rows;          // EPI 1: token of a sorted row;  EPI 2: pair of a sorted row
     const float* gates;             // EPI 2: factor per pair
-    void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N] fp32
+    // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N], 16-bit fixed point with a scale per row and block of kW8HBlock in out_scales (the
+    // wide kernels: fp32);  EPI 2: [pairs x N], the activations' type with out16, else fp32
+    void* out;
+    float* out_scales;
+    int out16;
     int act_bf16;
 };
 // The kernels of a product, named by rows x features of a workgroup (EPI 1: half as many output features, from gate and up).

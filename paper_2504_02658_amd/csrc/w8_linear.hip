@@ -94,6 +94,40 @@ int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream) {
     }
 }
 
+// Codes of rows in the 16-bit fixed point of the gate and up product: the row's largest value follows from its blocks' scales, so the rows
+// are read once.  Row-major output, zeros up to whole chunks.
+template <int TPR, int ROWS>
+__global__ __launch_bounds__(TPR * ROWS) void w8_requant_kernel(const int16_t* __restrict__ in, const float* __restrict__ block_scales, int64_t rows, int64_t K, int kb,
+                                                                uint8_t* __restrict__ codes, float* __restrict__ scales) {
+    const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (row >= rows) return;
+    const int nblk = (int)((K + kW8HBlock - 1) / kW8HBlock);
+    const float* const bs = block_scales + row * nblk;
+    uint32_t top = 0u;
+    for (int i = lane; i < nblk; i += 64) {
+        const uint32_t b = __float_as_uint(bs[i]);
+        top = b > top ? b : top;
+    }
+    const RowStep st = row_step(__float_as_uint(__uint_as_float(wave_max(top)) * 32767.0f) & 0x7fffffffu);
+    for (int p = tid; p < kb * 4; p += TPR) {
+        const int64_t k = (int64_t)p * 16;
+        const W8Raw<W8_F16> r = load16<W8_F16>(in + row * K, k, K);         // (16-bit elements)
+        const float f = k < K ? bs[k / kW8HBlock] * st.inv : 0.0f;
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = (float)(int16_t)(r.w[i >> 1] >> (16 * (i & 1)));
+        *reinterpret_cast<u32x4*>(codes + row * kb * 64 + k) = near_codes16(v, f);
+    }
+    if (tid == 0) scales[row] = st.s;
+}
+int launch_w8_requant(const int16_t* in, const float* block_scales, int64_t rows, int64_t K, uint8_t* codes, float* scales, hipStream_t stream) {
+    const int kb = (int)w8_kblocks(K);
+    if (kb * 4 <= 256) w8_requant_kernel<64, 16><<<dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, stream>>>(in, block_scales, rows, K, kb, codes, scales);
+    else w8_requant_kernel<256, 1><<<dim3((unsigned)rows), dim3(256), 0, stream>>>(in, block_scales, rows, K, kb, codes, scales);
+    return launch_status();
+}
+
 // The tiled product.
 template <int WM, int WN, int WK, int TM, int TN, int NS, int EPI, bool BF>
 __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8TileArgs a) {
@@ -239,9 +273,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
         for (; c + NS < stages; ++c) stage(std::bool_constant<true>{});
         for (; c < stages; ++c) stage(std::bool_constant<false>{});
     };
-    if (TM >= 4 && used >= 4) k_loop(std::integral_constant<int, TM >= 4 ? 4 : 1>{});
-    else if (TM >= 3 && used == 3) k_loop(std::integral_constant<int, TM >= 3 ? 3 : 1>{});
-    else if (TM >= 2 && used >= 2) k_loop(std::integral_constant<int, TM >= 2 ? 2 : 1>{});
+    static_assert(TM <= 2, "a loop for every number of blocks");
+    if (TM >= 2 && used >= 2) k_loop(std::integral_constant<int, TM >= 2 ? 2 : 1>{});
     else if (used >= 1) k_loop(std::integral_constant<int, 1>{});
     else k_loop(std::integral_constant<int, 0>{});          // (copies its share, and keeps the barriers)
     if constexpr (WK == 2) {
@@ -258,7 +291,6 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
                     for (int i = 0; i < 4; ++i) part[((n * TM + m) * 4 + i) * 64] = i32x4{acc[n][m][4 * i], acc[n][m][4 * i + 1], acc[n][m][4 * i + 2], acc[n][m][4 * i + 3]};
         }
         __syncthreads();
-        if (wk == 1) return;
 #pragma unroll
         for (int n = 0; n < TN; ++n)
 #pragma unroll
@@ -270,44 +302,111 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
                     for (int j = 0; j < 4; ++j) acc[n][m][4 * i + j] += v[j];
                 }
     }
-    // lane: row (of 32) l32, output features 8 i + 4 h + 0..3
-    const bool vec = (a.N & 3) == 0;
+    // Output.  A lane has features 8 i + 4 h + 0..3 of row l32 (of 32): stored from there, an instruction would touch 64 lines.  So the tile goes
+    // through LDS, which nobody reads any more, and leaves it by whole rows.
     const auto sw0 = global_float(w8_scales(w0, a.N, a.K)), sw1 = global_float(w8_scales(w1, a.N, a.K));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    auto each = [&](auto&& put) {       // put(row of the tile, column of the tile, four values)
 #pragma unroll
-    for (int m = 0; m < TM; ++m) {
-        const int r = (m * WM + wm) * 32 + l32;
-        if (r >= rows) continue;
-        const int64_t row = row0 + r;
-        float sx;
-        int64_t to = row;
-        if constexpr (EPI == 0) sx = a.a_scales[row];
-        else if constexpr (EPI == 1) sx = a.a_scales[a.x_rows[row]];
-        else {
-            to = a.x_rows[row];
-            sx = a.a_scales[row] * a.gates[to];
-        }
+        for (int m = 0; m < TM; ++m) {
+            const int r = (m * WM + wm) * 32 + l32;
+            if (r >= rows || wk != 0) continue;         // (with K in two halves, the first one's waves have the sums)
+            const int64_t row = row0 + r;
+            float sx;
+            if constexpr (EPI == 0) sx = a.a_scales[row];
+            else if constexpr (EPI == 1) sx = a.a_scales[a.x_rows[row]];
+            else sx = a.a_scales[row] * a.gates[a.x_rows[row]];
 #pragma unroll
-        for (int n = 0; n < (EPI == 1 ? TN / 2 : TN); ++n)
+            for (int n = 0; n < (EPI == 1 ? TN / 2 : TN); ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t col = n0 + (EPI == 1 ? wn * (TN / 2) + n : wn * TN + n) * 32 + 8 * i + 4 * h;
-                if (col >= a.N) continue;
-                const int left = (int)(a.N - col < 4 ? a.N - col : 4);
-                float v[4];
+                for (int i = 0; i < 4; ++i) {
+                    const int c = (EPI == 1 ? wn * (TN / 2) + n : wn * TN + n) * 32 + 8 * i + 4 * h;
+                    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (n0 + c < a.N) {         // (there are scales for whole blocks of 16)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[j] = (float)acc[n][m][4 * i + j] * sx * sw0[col + j];
-                    if constexpr (EPI == 1) v[j] = silu_times(v[j], (float)acc[n + TN / 2][m][4 * i + j] * sx * sw1[col + j]);
+                        for (int j = 0; j < 4; ++j) {
+                            v[j] = (float)acc[n][m][4 * i + j] * sx * sw0[n0 + c + j];
+                            if constexpr (EPI == 1) v[j] = silu_times(v[j], (float)acc[n + TN / 2][m][4 * i + j] * sx * sw1[n0 + c + j]);
+                        }
+                    }
+                    put(r, c, v);
                 }
-                if constexpr (EPI == 0) {
+        }
+    };
+    constexpr int threads = WM * WN * WK * 64;
+    const int tid = threadIdx.x;
+    if constexpr (EPI == 1) {
+        // 16-bit fixed point: a row's 128 features as multiples of 1/32767 of the largest of them.  The quantizer that follows wants codes of 1/127
+        // of the row's largest value, so this costs at most 1/516 of a code, and half of fp32's bytes (fp16 would overflow for large
+        // bf16 activations, bf16 would move every tenth code).
+        static_assert(OUTN == kW8HBlock, "a block per row of the tile");
+        float* const tile = reinterpret_cast<float*>(smem);
+        constexpr int PITCH = OUTN + 4;
+        static_assert(BM * PITCH * 4 <= NS * STAGE, "room for the tile");
+        each([&](int r, int c, const float (&v)[4]) { *reinterpret_cast<f32x4*>(tile + r * PITCH + c) = f32x4{v[0], v[1], v[2], v[3]}; });
+        __syncthreads();
+        const int nblk = (int)((a.N + OUTN - 1) / OUTN);
+        int16_t* const out = reinterpret_cast<int16_t*>(a.out);
+        for (int r = tid / 32; r < rows; r += threads / 32) {
+            const int c = (tid & 31) * 4;
+            const f32x4 v = *reinterpret_cast<const f32x4*>(tile + r * PITCH + c);
+            uint32_t top = 0u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = n0 + c + j < a.N ? v[j] : 0.0f;     // (a column that is none)
+                const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+                top = b > top ? b : top;
+            }
+#pragma unroll
+            for (int d = 16; d >= 1; d >>= 1) {
+                const uint32_t o = __shfl_xor(top, d, 64);
+                top = o > top ? o : top;
+            }
+            const float most = __uint_as_float(top), inv = most > 0x1p-111f ? 32767.0f / most : 0.0f;
+            int q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = (int)rintf(v[j] * inv);
+            int16_t* const to = out + (row0 + r) * a.N + n0 + c;
+            if ((a.N & 3) == 0 && n0 + c < a.N) {
+                *reinterpret_cast<u32x2*>(to) = u32x2{(uint32_t)(q[0] & 0xffff) | (uint32_t)q[1] << 16, (uint32_t)(q[2] & 0xffff) | (uint32_t)q[3] << 16};
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (n0 + c + j < a.N) to[j] = (int16_t)q[j];
+            }
+            if ((tid & 31) == 0) a.out_scales[(row0 + r) * nblk + nt] = most * (1.0f / 32767.0f);
+        }
+    } else {
+        const bool out32 = EPI == 2 && !a.out16;
+        if (out32 || (a.N & 7) != 0) {
+            const bool vec = (a.N & 3) == 0;
+            each([&](int r, int c, const float (&v)[4]) {
+                const int64_t col = n0 + c, to = EPI == 2 ? a.x_rows[row0 + r] : row0 + r;
+                if (col >= a.N) return;
+                const int left = (int)(a.N - col < 4 ? a.N - col : 4);
+                if (!out32) {
                     store4<BF>(reinterpret_cast<uint16_t*>(a.out) + to * a.N + col, v, left, vec);
                 } else {
-                    float* o = reinterpret_cast<float*>(a.out) + to * a.N + col;
+                    float* const o = reinterpret_cast<float*>(a.out) + to * a.N + col;
                     if (vec) *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
                     else
                         for (int j = 0; j < left; ++j) o[j] = v[j];
                 }
+            });
+        } else {
+            uint16_t* const tile = reinterpret_cast<uint16_t*>(smem);
+            constexpr int PITCH = BN + 8;
+            static_assert(BM * PITCH * 2 <= NS * STAGE, "room for the tile");
+            each([&](int r, int c, const float (&v)[4]) { store4<BF>(tile + r * PITCH + c, v, 4, true); });
+            __syncthreads();
+            for (int r = tid / (BN / 8); r < rows; r += threads / (BN / 8)) {
+                const int c = (tid % (BN / 8)) * 8;
+                if (n0 + c >= a.N) continue;
+                const int64_t to = EPI == 2 ? a.x_rows[row0 + r] : row0 + r;
+                *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.out) + to * a.N + n0 + c) = *reinterpret_cast<const u32x4*>(tile + r * PITCH + c);
             }
+        }
     }
 }
 
@@ -325,17 +424,19 @@ static int launch_tile(W8TileArgs a, hipStream_t stream) {
     w8_tile_kernel<WM, WN, WK, TM, TN, NS, EPI, BF><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(WM * WN * WK * 64), lds, stream>>>(a);
     return launch_status();
 }
-template <int EPI, bool BF>
-static int launch_tile_shape(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
+template <bool BF>
+static int launch_linear_tile(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
     switch (k) {
-        case W8_TILE_64x128: return launch_tile<2, 2, 2, 1, 2, 4, EPI, BF>(a, stream);
-        case W8_TILE_128x128: return launch_tile<2, 2, 1, 2, 2, 4, EPI, BF>(a, stream);
-        default: return launch_tile<2, 4, 1, 2, 2, 3, EPI, BF>(a, stream);      // (72 KB of LDS: two workgroups share a compute unit)
+        case W8_TILE_64x128: return launch_tile<2, 2, 2, 1, 2, 4, 0, BF>(a, stream);
+        case W8_TILE_128x128: return launch_tile<2, 2, 1, 2, 2, 4, 0, BF>(a, stream);
+        default: return launch_tile<2, 4, 1, 2, 2, 3, 0, BF>(a, stream);        // (72 KB of LDS: two workgroups share a compute unit)
     }
 }
 static int launch_w8_tile(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream) {
-    if (epi == 0) return a.act_bf16 ? launch_tile_shape<0, true>(a, k, stream) : launch_tile_shape<0, false>(a, k, stream);
-    return epi == 1 ? launch_tile_shape<1, false>(a, k, stream) : launch_tile_shape<2, false>(a, k, stream);
+    if (epi == 0) return a.act_bf16 ? launch_linear_tile<true>(a, k, stream) : launch_linear_tile<false>(a, k, stream);
+    if (k != W8_TILE_128x256) return MILO_ERR_SHAPE;        // (experts: this one alone)
+    if (epi == 1) return launch_tile<2, 4, 1, 2, 2, 3, 1, false>(a, stream);
+    return a.act_bf16 ? launch_tile<2, 4, 1, 2, 2, 3, 2, true>(a, stream) : launch_tile<2, 4, 1, 2, 2, 3, 2, false>(a, stream);
 }
 int w8_kernel_rows(W8Kernel k) {
     switch (k) {

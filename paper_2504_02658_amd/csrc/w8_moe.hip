@@ -378,9 +378,10 @@ static int launch_few(const W8FewArgs& a, hipStream_t s) {
 
 // ---------------------------------------------------------------------------------------------
 // Y = sum over a token's pairs of their rows of O, in slot order; a pair whose id is out of range has none.
-template <bool BF>
-__global__ __launch_bounds__(256) void w8_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ ids, int topk, int E, int64_t H,
+template <bool BF, bool OUT16>
+__global__ __launch_bounds__(256) void w8_combine_kernel(const void* __restrict__ O, const int32_t* __restrict__ ids, int topk, int E, int64_t H,
                                                          uint16_t* __restrict__ Y) {
+    constexpr int IN = OUT16 ? (BF ? W8_BF16 : W8_F16) : W8_F32;
     const int64_t t = blockIdx.x;
     for (int64_t h = (int64_t)threadIdx.x * 4; h < H; h += 1024) {
         const int left = (int)(H - h < 4 ? H - h : 4);
@@ -388,21 +389,34 @@ __global__ __launch_bounds__(256) void w8_combine_kernel(const float* __restrict
         for (int j = 0; j < topk; ++j) {
             const int64_t p = t * topk + j;
             if ((uint32_t)ids[p] >= (uint32_t)E) continue;
-            const float* const o = O + p * H + h;
+            const char* const o = reinterpret_cast<const char*>(O) + (p * H + h) * (OUT16 ? 2 : 4);
+            W8Raw<IN> r = {};
+            if (left == 4) {
+                __builtin_memcpy(&r, o, OUT16 ? 8 : 16);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < left) v[i] += o[i];
+                for (int i = 0; i < 4; ++i)
+                    if (i < left) {
+                        if constexpr (OUT16) r.w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(o)[i] << (16 * (i & 1));
+                        else r.w[i] = reinterpret_cast<const uint32_t*>(o)[i];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += raw_value<IN>(r, i);
         }
         store4<BF>(Y + t * H + h, v, left, (H & 3) == 0);
     }
 }
+
+constexpr int64_t kPairsFp32 = 64 << 20;        // bytes
 
 // Workspace of a forward.
 struct W8MoeLayout {
     bool few;
     W8Kernel kernel;
     int bm, max_tiles;
-    size_t off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
+    bool fixed_h, out16;        // H in 16-bit fixed point; the pairs' outputs in the activations' type
+    size_t off_hblk, off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
 };
 static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8MoeLayout* L) {
     if (T < 1 || E < 1 || E > 65536 || topk < 1 || topk > E) return false;
@@ -419,7 +433,11 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         return at;
     };
     L->few = T <= kFewTokens && P <= kFewMaxPairs;
-    L->off_h = take((size_t)P * F * 4);
+    // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest (66 experts of
+    // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256; 8 experts of 14336 x 4096, 64 tokens: 331 against 300).
+    L->kernel = P < 12 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
+    L->fixed_h = !L->few && L->kernel == W8_TILE_128x256;
+    L->off_h = take((size_t)P * F * (L->fixed_h ? 2 : 4));
     L->off_xq = take((size_t)(T * hb));
     L->off_xs = take((size_t)T * 4);
     if (L->few) {
@@ -427,18 +445,18 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         L->off_hq = take((size_t)(P * fb));
         L->off_hs = take((size_t)P * 4);
     } else {
-        // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest (66 experts of
-        // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256; 8 experts of 14336 x 4096, 64 tokens: 331 against 300).
-        const int64_t met = P < E ? P : E;
-        L->kernel = P < 12 * met ? W8_WIDE_32x64 : W8_TILE_128x256;
         L->bm = w8_kernel_rows(L->kernel);
+        // A pair's weighted output is kept in fp32 while all of them fit the caches; beyond, in the activations' type (half of a step of it
+        // per pair, as the output itself): 4096 tokens to 8 experts of 2048 features each, OUT16_TIMES.
+        L->out16 = L->kernel == W8_TILE_128x256 && P * H * 4 > kPairsFp32;
+        if (L->fixed_h) L->off_hblk = take((size_t)P * ((F + kW8HBlock - 1) / kW8HBlock) * 4);
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
         L->off_sorted = take((size_t)P * 4);
         L->off_token = take((size_t)P * 4);
         L->off_tiles = take((size_t)L->max_tiles * sizeof(TileDesc));
         L->off_hq = take((size_t)(P * fb));
         L->off_hs = take((size_t)P * 4);
-        L->off_o = take((size_t)P * H * 4);
+        L->off_o = take((size_t)P * H * (L->out16 ? 2 : 4));
     }
     L->total = off;
     return true;
@@ -530,6 +548,9 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.m_tiles = L.max_tiles;
     t.x_rows = g.sorted_token;
     t.out = ws + L.off_h;
+    if (L.fixed_h) t.out_scales = reinterpret_cast<float*>(ws + L.off_hblk);
+    t.act_bf16 = bf;
+    t.out16 = L.out16;
     st = launch_w8_product(t, 1, L.kernel, s);
     if (st != MILO_OK) return st;
     q.in = ws + L.off_h;
@@ -537,7 +558,8 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     q.K = F;
     q.codes = reinterpret_cast<uint8_t*>(ws + L.off_hq);
     q.scales = reinterpret_cast<float*>(ws + L.off_hs);
-    st = launch_w8_quant(q, W8_F32, s);
+    if (L.fixed_h) st = launch_w8_requant(reinterpret_cast<const int16_t*>(ws + L.off_h), t.out_scales, P, F, q.codes, q.scales, s);
+    else st = launch_w8_quant(q, W8_F32, s);
     if (st != MILO_OK) return st;
     t.A = q.codes;
     t.a_bytes = (uint64_t)(P * w8_kblocks(F) * 64);
@@ -549,8 +571,8 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.out = ws + L.off_o;
     st = launch_w8_product(t, 2, L.kernel, s);
     if (st != MILO_OK) return st;
-    const float* const O = reinterpret_cast<const float*>(ws + L.off_o);
-    if (bf) w8_combine_kernel<true><<<dim3((unsigned)T), dim3(256), 0, s>>>(O, topk_ids, topk, E, H, Y);
-    else w8_combine_kernel<false><<<dim3((unsigned)T), dim3(256), 0, s>>>(O, topk_ids, topk, E, H, Y);
+    auto combine = [&](auto kernel) { kernel<<<dim3((unsigned)T), dim3(256), 0, s>>>(ws + L.off_o, topk_ids, topk, E, H, Y); };
+    if (bf) combine(L.out16 ? w8_combine_kernel<true, true> : w8_combine_kernel<true, false>);
+    else combine(L.out16 ? w8_combine_kernel<false, true> : w8_combine_kernel<false, false>);
     return launch_status();
 }
