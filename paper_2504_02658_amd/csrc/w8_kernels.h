@@ -22,9 +22,6 @@ struct W8QuantArgs {
 };
 int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream);
 
-constexpr int kW8HBlock = 128;
-int launch_w8_requant(const int16_t* in, const float* block_scales, int64_t rows, int64_t K, uint8_t* codes, float* scales, hipStream_t stream);
-
 // Tiled product.  Row r of a tile's A operand:
 //   EPI 0 (a linear):         blocked activations, row 'tile * BM + r' of M
 //   EPI 1 (gate and up):      row-major activations, row x_rows[row0 + r]
@@ -40,10 +37,7 @@ struct W8TileArgs {
     int m_tiles, n_tiles;           // EPI 1, 2: m_tiles slots, some of them empty; the rest is set at the launch
     const int32_t* x_rows;          // EPI 1: token of a sorted row;  EPI 2: pair of a sorted row
     const float* gates;             // EPI 2: factor per pair
-    // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N], 16-bit fixed point with a scale per row and block of kW8HBlock in out_scales (the
-    // wide kernels: fp32);  EPI 2: [pairs x N], the activations' type with out16, else fp32
-    void* out;
-    float* out_scales;
+    void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N], the activations' type with out16, else fp32
     int out16;
     int act_bf16;
 };
@@ -51,6 +45,11 @@ struct W8TileArgs {
 enum W8Kernel { W8_WIDE_16x16, W8_WIDE_16x32, W8_WIDE_16x64, W8_WIDE_32x32, W8_WIDE_32x64, W8_WIDE_64x64, W8_TILE_64x128, W8_TILE_128x128, W8_TILE_128x256 };
 int w8_kernel_rows(W8Kernel k);
 int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream);
+// Up to 16 rows whose codes fit kW8WideStaged bytes, in one launch: a.A is the 16-bit activations, k one of the kernels of 16 rows.  (Every
+// workgroup quantizes all rows: N = 14336, K = 4096 takes 15.3 us in one launch against 17.6 in two for one row, 15.4 / 18.0 for four, 19.5 /
+// 17.4 for eight; 16 rows of 1024 x 1024 5.9 / 8.0.)
+constexpr int kW8WideStaged = 16 * 1024;
+int launch_w8_staged(const W8TileArgs& a, W8Kernel k, hipStream_t stream);
 int launch_w8_wide(const W8TileArgs& a, int epi, int tm, int rn, hipStream_t stream);      // w8_wide.hip: 16 tm x 16 rn
 
 

@@ -94,40 +94,6 @@ int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream) {
     }
 }
 
-// Codes of rows in the 16-bit fixed point of the gate and up product: the row's largest value follows from its blocks' scales, so the rows
-// are read once.  Row-major output, zeros up to whole chunks.
-template <int TPR, int ROWS>
-__global__ __launch_bounds__(TPR * ROWS) void w8_requant_kernel(const int16_t* __restrict__ in, const float* __restrict__ block_scales, int64_t rows, int64_t K, int kb,
-                                                                uint8_t* __restrict__ codes, float* __restrict__ scales) {
-    const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-    if (row >= rows) return;
-    const int nblk = (int)((K + kW8HBlock - 1) / kW8HBlock);
-    const float* const bs = block_scales + row * nblk;
-    uint32_t top = 0u;
-    for (int i = lane; i < nblk; i += 64) {
-        const uint32_t b = __float_as_uint(bs[i]);
-        top = b > top ? b : top;
-    }
-    const RowStep st = row_step(__float_as_uint(__uint_as_float(wave_max(top)) * 32767.0f) & 0x7fffffffu);
-    for (int p = tid; p < kb * 4; p += TPR) {
-        const int64_t k = (int64_t)p * 16;
-        const W8Raw<W8_F16> r = load16<W8_F16>(in + row * K, k, K);         // (16-bit elements)
-        const float f = k < K ? bs[k / kW8HBlock] * st.inv : 0.0f;
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = (float)(int16_t)(r.w[i >> 1] >> (16 * (i & 1)));
-        *reinterpret_cast<u32x4*>(codes + row * kb * 64 + k) = near_codes16(v, f);
-    }
-    if (tid == 0) scales[row] = st.s;
-}
-int launch_w8_requant(const int16_t* in, const float* block_scales, int64_t rows, int64_t K, uint8_t* codes, float* scales, hipStream_t stream) {
-    const int kb = (int)w8_kblocks(K);
-    if (kb * 4 <= 256) w8_requant_kernel<64, 16><<<dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, stream>>>(in, block_scales, rows, K, kb, codes, scales);
-    else w8_requant_kernel<256, 1><<<dim3((unsigned)rows), dim3(256), 0, stream>>>(in, block_scales, rows, K, kb, codes, scales);
-    return launch_status();
-}
-
 // The tiled product.
 template <int WM, int WN, int WK, int TM, int TN, int NS, int EPI, bool BF>
 __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8TileArgs a) {
@@ -337,45 +303,25 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
     constexpr int threads = WM * WN * WK * 64;
     const int tid = threadIdx.x;
     if constexpr (EPI == 1) {
-        // 16-bit fixed point: a row's 128 features as multiples of 1/32767 of the largest of them.  The quantizer that follows wants codes of 1/127
-        // of the row's largest value, so this costs at most 1/516 of a code, and half of fp32's bytes (fp16 would overflow for large
-        // bf16 activations, bf16 would move every tenth code).
-        static_assert(OUTN == kW8HBlock, "a block per row of the tile");
+        // fp32: the quantizer that follows has to see the value that it rounds.  (16-bit fixed point with a scale per row and 128 features moves
+        // one code in 600, and one step of a code in 600 is 0.16 % of the layer's output, eight times what fp16 rounds off; it took 35 us
+        // less of 540, 4096 tokens of 66 experts of 1408.)
         float* const tile = reinterpret_cast<float*>(smem);
-        constexpr int PITCH = OUTN + 4;
+        constexpr int PITCH = OUTN + 4, Q = OUTN / 4;
         static_assert(BM * PITCH * 4 <= NS * STAGE, "room for the tile");
         each([&](int r, int c, const float (&v)[4]) { *reinterpret_cast<f32x4*>(tile + r * PITCH + c) = f32x4{v[0], v[1], v[2], v[3]}; });
         __syncthreads();
-        const int nblk = (int)((a.N + OUTN - 1) / OUTN);
-        int16_t* const out = reinterpret_cast<int16_t*>(a.out);
-        for (int r = tid / 32; r < rows; r += threads / 32) {
-            const int c = (tid & 31) * 4;
+        for (int r = tid / Q; r < rows; r += threads / Q) {
+            const int c = (tid % Q) * 4;
             const f32x4 v = *reinterpret_cast<const f32x4*>(tile + r * PITCH + c);
-            uint32_t top = 0u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = n0 + c + j < a.N ? v[j] : 0.0f;     // (a column that is none)
-                const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-                top = b > top ? b : top;
-            }
-#pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) {
-                const uint32_t o = __shfl_xor(top, d, 64);
-                top = o > top ? o : top;
-            }
-            const float most = __uint_as_float(top), inv = most > 0x1p-111f ? 32767.0f / most : 0.0f;
-            int q[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = (int)rintf(v[j] * inv);
-            int16_t* const to = out + (row0 + r) * a.N + n0 + c;
-            if ((a.N & 3) == 0 && n0 + c < a.N) {
-                *reinterpret_cast<u32x2*>(to) = u32x2{(uint32_t)(q[0] & 0xffff) | (uint32_t)q[1] << 16, (uint32_t)(q[2] & 0xffff) | (uint32_t)q[3] << 16};
+            float* const to = reinterpret_cast<float*>(a.out) + (row0 + r) * a.N + n0 + c;
+            if ((a.N & 3) == 0) {
+                if (n0 + c < a.N) *reinterpret_cast<f32x4*>(to) = v;
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (n0 + c + j < a.N) to[j] = (int16_t)q[j];
+                    if (n0 + c + j < a.N) to[j] = v[j];
             }
-            if ((tid & 31) == 0) a.out_scales[(row0 + r) * nblk + nt] = most * (1.0f / 32767.0f);
         }
     } else {
         const bool out32 = EPI == 2 && !a.out16;
@@ -532,6 +478,18 @@ extern "C" int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t 
     if (!workspace || workspace_bytes < milo_w8a8_gemm_workspace(M, N, K)) return MILO_ERR_WORKSPACE;
     if (!aligned16(X) || !aligned16(w8) || !aligned16(Y) || !aligned16(workspace)) return MILO_ERR_ALIGN;
     const bool bf = (flags & MILO_ACT_BF16) != 0;
+    const W8Kernel kernel = w8_linear_kernel(M, N, K);
+    W8TileArgs a = {};
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    a.w = w8;
+    a.out = Y;
+    a.act_bf16 = bf;
+    if (M <= 16 && M * w8_kblocks(K) * 64 <= kW8WideStaged) {
+        a.A = reinterpret_cast<const uint8_t*>(X);
+        return launch_w8_staged(a, kernel, (hipStream_t)stream);
+    }
     W8QuantArgs q;
     q.in = X;
     q.rows = M;
@@ -539,19 +497,12 @@ extern "C" int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t 
     q.codes = reinterpret_cast<uint8_t*>(workspace);
     q.scales = reinterpret_cast<float*>(q.codes + gemm_scales_off(M, K));
     q.blocked = 1;
-    int st = launch_w8_quant(q, bf ? W8_BF16 : W8_F16, (hipStream_t)stream);
+    const int st = launch_w8_quant(q, bf ? W8_BF16 : W8_F16, (hipStream_t)stream);
     if (st != MILO_OK) return st;
-    W8TileArgs a = {};
     a.A = q.codes;
     a.a_bytes = (uint64_t)w8_code_bytes(M, K);
     a.a_scales = q.scales;
-    a.M = M;
-    a.N = N;
-    a.K = K;
-    a.w = w8;
-    a.out = Y;
-    a.act_bf16 = bf;
-    return launch_w8_product(a, 0, w8_linear_kernel(M, N, K), (hipStream_t)stream);
+    return launch_w8_product(a, 0, kernel, (hipStream_t)stream);
 }
 
 // For the tests: which kernel a linear takes (W8Kernel; for the current device, or without one for 256 compute units).

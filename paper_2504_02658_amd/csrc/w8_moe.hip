@@ -415,8 +415,8 @@ struct W8MoeLayout {
     bool few;
     W8Kernel kernel;
     int bm, max_tiles;
-    bool fixed_h, out16;        // H in 16-bit fixed point; the pairs' outputs in the activations' type
-    size_t off_hblk, off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
+    bool out16;                 // the pairs' outputs in the activations' type
+    size_t off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
 };
 static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8MoeLayout* L) {
     if (T < 1 || E < 1 || E > 65536 || topk < 1 || topk > E) return false;
@@ -436,8 +436,7 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest (66 experts of
     // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256; 8 experts of 14336 x 4096, 64 tokens: 331 against 300).
     L->kernel = P < 12 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
-    L->fixed_h = !L->few && L->kernel == W8_TILE_128x256;
-    L->off_h = take((size_t)P * F * (L->fixed_h ? 2 : 4));
+    L->off_h = take((size_t)P * F * 4);
     L->off_xq = take((size_t)(T * hb));
     L->off_xs = take((size_t)T * 4);
     if (L->few) {
@@ -447,9 +446,8 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     } else {
         L->bm = w8_kernel_rows(L->kernel);
         // A pair's weighted output is kept in fp32 while all of them fit the caches; beyond, in the activations' type (half of a step of it
-        // per pair, as the output itself): 4096 tokens to 8 experts of 2048 features each, OUT16_TIMES.
+        // per pair, as the output itself): 4096 tokens to 8 experts each, 2048 features, 268 MB of fp32: 611 us for the layer against 702.
         L->out16 = L->kernel == W8_TILE_128x256 && P * H * 4 > kPairsFp32;
-        if (L->fixed_h) L->off_hblk = take((size_t)P * ((F + kW8HBlock - 1) / kW8HBlock) * 4);
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
         L->off_sorted = take((size_t)P * 4);
         L->off_token = take((size_t)P * 4);
@@ -548,7 +546,6 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.m_tiles = L.max_tiles;
     t.x_rows = g.sorted_token;
     t.out = ws + L.off_h;
-    if (L.fixed_h) t.out_scales = reinterpret_cast<float*>(ws + L.off_hblk);
     t.act_bf16 = bf;
     t.out16 = L.out16;
     st = launch_w8_product(t, 1, L.kernel, s);
@@ -558,8 +555,7 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     q.K = F;
     q.codes = reinterpret_cast<uint8_t*>(ws + L.off_hq);
     q.scales = reinterpret_cast<float*>(ws + L.off_hs);
-    if (L.fixed_h) st = launch_w8_requant(reinterpret_cast<const int16_t*>(ws + L.off_h), t.out_scales, P, F, q.codes, q.scales, s);
-    else st = launch_w8_quant(q, W8_F32, s);
+    st = launch_w8_quant(q, W8_F32, s);
     if (st != MILO_OK) return st;
     t.A = q.codes;
     t.a_bytes = (uint64_t)(P * w8_kblocks(F) * 64);

@@ -6,6 +6,9 @@
 // loop through LDS takes a quarter of a microsecond per 64 columns whatever it multiplies there, when a compute unit has one
 // workgroup.  What bounds it is the weight's bytes while there is one tile of rows, then the 64 bytes per cycle that a compute unit
 // gets from its cache: (TM + RN) KB per 64 columns for TM RN matrix instructions.
+//
+// STAGED: up to 16 rows of a linear in their 16-bit type, which every workgroup quantizes for itself into LDS while its first fragments are
+// on their way; so such a call is one launch.
 #include "milo_host.h"
 #include "w8_kernels.h"
 
@@ -13,13 +16,17 @@ namespace milo {
 
 constexpr int kWideWaves = 8;
 
-template <int TM, int RN, int EPI, bool BF>
+template <int TM, int RN, int EPI, bool BF, bool STAGED>
 __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8TileArgs a) {
     constexpr int NW = kWideWaves, B = TM + RN <= 2 ? 4 : TM + RN <= 4 ? 2 : 1;      // units (of 64 columns) of a step
     constexpr int OUTN = 16 * (EPI == 1 ? RN / 2 : RN);
     static_assert(EPI != 1 || RN % 2 == 0, "gate and up");
+    static_assert(!STAGED || (EPI == 0 && TM == 1), "rows of a linear");
+    constexpr int IN = BF ? W8_BF16 : W8_F16;
+    __shared__ uint32_t s_top[STAGED ? 16 : 1][NW];
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     i32x4* const s_part = reinterpret_cast<i32x4*>(smem);           // [wave][tile][lane]
+    unsigned char* const codes = smem + NW * TM * RN * 1024;        // STAGED: piece c of 16 columns of row m at (c * rows + m) * 16
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m16 = lane & 15, c16 = lane >> 4;
     const int kb = (int)w8_kblocks(a.K);
@@ -69,8 +76,10 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
             const int v = u + i < kb ? u + i : kb - 1;
 #pragma unroll
             for (int n = 0; n < RN; ++n) wf[to][i][n] = wp[n][v * 64];
+            if constexpr (!STAGED) {
 #pragma unroll
-            for (int m = 0; m < TM; ++m) xf[to][i][m] = xp[m][v * XSTEP];
+                for (int m = 0; m < TM; ++m) xf[to][i][m] = xp[m][v * XSTEP];
+            }
         }
     };
     i32x4 acc[TM][RN];
@@ -79,6 +88,14 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
 #pragma unroll
         for (int n = 0; n < RN; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
     auto work = [&](int u, int from) {
+        if constexpr (STAGED) {
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                const int v = u + i < kb ? u + i : kb - 1;
+                xf[from][i][0] = u32x4{0u, 0u, 0u, 0u};
+                if (m16 < rows) xf[from][i][0] = *reinterpret_cast<const u32x4*>(codes + ((v * 4 + c16) * rows + m16) * 16);
+            }
+        }
         fetch(u + B * NW, from ^ 1);
         asm volatile("" ::: "memory");              // (the loads stay in front)
         __builtin_amdgcn_sched_barrier(0);
@@ -92,6 +109,29 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
         }
     };
     if (wave * B < kb) fetch(wave * B, 0);
+    if constexpr (STAGED) {
+        // up to eight waves share a row
+        const int share = rows > 4 ? 1 : rows > 2 ? 2 : rows > 1 ? 4 : 8, part = wave % share, pieces = kb * 4;
+        const char* const X = reinterpret_cast<const char*>(a.A);
+        for (int m = wave / share; m < rows; m += NW / share) {
+            uint32_t top = 0u;
+            for (int p = part * 64 + lane; p < pieces; p += share * 64) top = raw_top<IN>(load16<IN>(X + m * a.K * 2, (int64_t)p * 16, a.K), top);
+            top = wave_max(top);
+            if (lane == 0) s_top[m][part] = top;
+        }
+        __syncthreads();
+        for (int m = wave / share; m < rows; m += NW / share) {
+            uint32_t top = s_top[m][0];
+            for (int i = 1; i < share; ++i) top = s_top[m][i] > top ? s_top[m][i] : top;
+            const RowStep st = row_step(top);
+            for (int p = part * 64 + lane; p < pieces; p += share * 64) {
+                float v[16];
+                raw_values<IN>(load16<IN>(X + m * a.K * 2, (int64_t)p * 16, a.K), v);
+                *reinterpret_cast<u32x4*>(codes + (p * rows + m) * 16) = row_codes16(v, st);
+            }
+        }
+        __syncthreads();
+    }
     for (int u = wave * B; u < kb; u += 2 * B * NW) {
         work(u, 0);
         if (u + B * NW >= kb) break;
@@ -123,7 +163,12 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
         const int left = (int)(a.N - col < 4 ? a.N - col : 4);
         int64_t to = row;
         float sx;
-        if constexpr (EPI == 0) sx = a.a_scales[row];
+        if constexpr (STAGED) {
+            const int share = rows > 4 ? 1 : rows > 2 ? 2 : rows > 1 ? 4 : 8;
+            uint32_t top = s_top[r][0];
+            for (int i = 1; i < share; ++i) top = s_top[r][i] > top ? s_top[r][i] : top;
+            sx = row_step(top).s;
+        } else if constexpr (EPI == 0) sx = a.a_scales[row];
         else if constexpr (EPI == 1) sx = a.a_scales[a.x_rows[row]];
         else {
             to = a.x_rows[row];
@@ -146,18 +191,19 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
     }
 }
 
-template <int TM, int RN, int EPI, bool BF>
+template <int TM, int RN, int EPI, bool BF, bool STAGED = false>
 static int launch_wide(W8TileArgs a, hipStream_t stream) {
-    constexpr int OUTN = 16 * (EPI == 1 ? RN / 2 : RN), lds = kWideWaves * TM * RN * 1024;
-    if constexpr (lds > 64 * 1024) {
+    constexpr int OUTN = 16 * (EPI == 1 ? RN / 2 : RN), most = kWideWaves * TM * RN * 1024 + (STAGED ? kW8WideStaged : 0);
+    const int lds = kWideWaves * TM * RN * 1024 + (STAGED ? (int)(a.M * w8_kblocks(a.K) * 64) : 0);
+    if constexpr (most > 64 * 1024) {
         static bool raised[64] = {false};
-        const int st = raise_lds(reinterpret_cast<const void*>(w8_wide_kernel<TM, RN, EPI, BF>), lds, raised);
+        const int st = raise_lds(reinterpret_cast<const void*>(w8_wide_kernel<TM, RN, EPI, BF, STAGED>), most, raised);
         if (st != MILO_OK) return st;
     }
     if (EPI == 0) a.m_tiles = (int)((a.M + TM * 16 - 1) / (TM * 16));
     a.n_tiles = (int)((a.N + OUTN - 1) / OUTN);
     if ((int64_t)a.m_tiles * a.n_tiles > (int64_t(1) << 31) / (kWideWaves * 64)) return MILO_ERR_SHAPE;
-    w8_wide_kernel<TM, RN, EPI, BF><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(kWideWaves * 64), lds, stream>>>(a);
+    w8_wide_kernel<TM, RN, EPI, BF, STAGED><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(kWideWaves * 64), lds, stream>>>(a);
     return launch_status();
 }
 template <int EPI, bool BF>
@@ -168,6 +214,15 @@ static int launch_wide_shape(const W8TileArgs& a, int tm, int rn, hipStream_t st
     if (tm == 2) return rn == 4 ? launch_wide<2, 4, EPI, BF>(a, stream) : launch_wide<2, 2, EPI, BF>(a, stream);
     if (rn == 4) return launch_wide<1, 4, EPI, BF>(a, stream);
     return rn == 2 || EPI == 1 ? launch_wide<1, 2, EPI, BF>(a, stream) : launch_wide<1, EPI == 1 ? 2 : 1, EPI, BF>(a, stream);
+}
+template <bool BF>
+static int launch_staged(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
+    if (k == W8_WIDE_16x64) return launch_wide<1, 4, 0, BF, true>(a, stream);
+    if (k == W8_WIDE_16x32) return launch_wide<1, 2, 0, BF, true>(a, stream);
+    return launch_wide<1, 1, 0, BF, true>(a, stream);
+}
+int launch_w8_staged(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
+    return a.act_bf16 ? launch_staged<true>(a, k, stream) : launch_staged<false>(a, k, stream);
 }
 int launch_w8_wide(const W8TileArgs& a, int epi, int tm, int rn, hipStream_t stream) {
     if (epi == 0) return a.act_bf16 ? launch_wide_shape<0, true>(a, tm, rn, stream) : launch_wide_shape<0, false>(a, tm, rn, stream);

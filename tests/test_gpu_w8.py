@@ -5,8 +5,8 @@ Linear: the integer sum is exact; turning it into fp32, the two products with th
 give |err| <= |y| (u + 4 v), plus half the smallest subnormal of fp16.
 Layer: a pair's gate and up values carry at most 3 v each and SiLU(a) b then less than 2^-18 (|a| 3 v through the
 sigmoid, exp and the quotient a few v each, for |a| up to 16); with the scale's own rounding a quotient h / step of at most
-127 is off by less than 2^-10, and by 2^-9 more where the rows lie in 16-bit fixed point between the two products.  So codes
-within 2^-8 of a border may differ (the oracle sums their effect), all others may not, and the steps move a term by less than 2^-15.
+127 is off by less than 2^-10.  So codes
+within 2^-10 of a border may differ (the oracle sums their effect), all others may not, and the steps move a term by less than 2^-15.
 A term kept in the activations' type adds u of itself.  Sums over the pairs add 2^-15 of the terms' magnitudes generously.
 """
 import numpy as np
@@ -280,7 +280,7 @@ def routing(T, E, k, seed):
 
 
 def check_layer(Y, X, host, ids, gates, kept16=False):
-    ref, doubt, terms = oracle.w8a8_moe(X.float().numpy(), host, ids.numpy(), gates.numpy(), border=2.0 ** -8)
+    ref, doubt, terms = oracle.w8a8_moe(X.float().numpy(), host, ids.numpy(), gates.numpy(), border=2.0 ** -10)
     # The sum before its rounding lies within d of ref, and the rounding moves it by at most u of itself: |err| <= d + u (|ref| + d).  (Without
     # the last d: 64 x 256 x 256, bf16, one term of 0.0030 whose only doubtful code made it 0.0051, u of the difference short.)
     u = U[Y.dtype]

@@ -105,7 +105,7 @@ def test_layer_of_large_and_small_values(api, T):
         X = normal(T, (T, H), torch.bfloat16)
         ids, gates = routing(T, E, 2, seed=1)
         Y = layer.forward(X.cuda(), ids.cuda(), gates.cuda())
-        ref, doubt, terms = oracle.w8a8_moe(X.float().numpy(), host, ids.numpy(), gates.numpy(), border=2.0 ** -8)
+        ref, doubt, terms = oracle.w8a8_moe(X.float().numpy(), host, ids.numpy(), gates.numpy(), border=2.0 ** -8)        # (127 times the 2^-15 below)
         # a gate value of magnitude |a| enters the sigmoid with 3 steps of fp32, so SiLU(a) b carries up to |a| 2^-22: 2^-9 at 2^13
         # where the sigmoid is not yet 0 or 1 it is below 90: 2^-15
         d = doubt + terms * 2.0 ** -13
