@@ -381,8 +381,8 @@ int milo_moe_w3lr_routing_status(const void* workspace, void* stream);
  * with the sum exact in 32-bit integers (whatever the order), its products with the scales in fp32 and one rounding to
  * the output type.  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale
  * NaN, so that what is computed from it is NaN and nothing else is touched.
- * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M <= 2^23 and N K, M K <= 2^40; nothing has to be a
- * multiple of anything.  Pointers are 16-byte aligned, arrays dense.  These calls need no prepared workspace: theirs is scratch
+ * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M < 2^22, N K, M K <= 2^40 and M N <= 2^36; nothing has to
+ * be a multiple of anything.  Pointers are 16-byte aligned, arrays dense.  These calls need no prepared workspace: theirs is scratch
  * alone, may hold anything before and after, and keeps nothing between calls; no kernel of theirs waits for another workgroup,
  * so that they run beside other streams' work and can be captured in a graph.
  *
@@ -421,7 +421,7 @@ int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t K, const vo
  * milo_moe_w8a8_forward take.  The logits are formed and compared in 64 bits, so the choice does not depend on the order of
  * the summation.  A NaN logit ranks below every other one (the ids stay distinct and in range) and makes all gates of its token NaN;
  * so does an infinite largest logit.
- * Limits: E <= 1024, topk <= min(E, 64), n_shared <= 64, T <= 2^23, H <= 2^20.
+ * Limits: E <= 1024, topk <= min(E, 64), n_shared <= 64, T < 2^22, H <= 2^20.
  * Errors: NULL, SHAPE (also unknown flags), ALIGN, HIP.
  */
 #define MILO_ROUTE_RENORMALIZE 8u
@@ -440,8 +440,9 @@ int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H,
  * Top-k routed MoE feed-forward layer over W8A8 experts:
  *     y_t = sum_j gates[t,j] * lin_w2^e( SiLU(lin_w1^e(x_t)) * lin_w3^e(x_t) ),   e = ids[t,j]
  * with every lin the W8A8 linear above: a token's activations are quantized once, the SwiGLU output of a (token, expert) pair is
- * a row of its own, and it is quantized from fp32.  Up to 16 tokens (128 pairs) two launches, reading the weights of the experts
- * that occur; more tokens are grouped per expert inside the call.
+ * a row of its own, and it is quantized from fp32.  Up to 16 tokens (128 pairs) two products and nothing else, reading the weights of the experts that
+ * occur (two launches; with more activations than the products quantize for themselves, three or four); more tokens are grouped per
+ * expert inside the call.
  *   X  [T x H] fp16, or bfloat16 with MILO_ACT_BF16;  Y the same
  *   experts      DEVICE array of E entries (a byte copy of a table that passed milo_moe_w8a8_check_experts)
  *   topk_ids     [T x topk] int32, topk <= E, the ids of one token distinct;  topk_weights  [T x topk] fp32
@@ -449,7 +450,9 @@ int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H,
  *   workspace    milo_moe_w8a8_workspace(T, H, F, E, topk) bytes (0 if the shape is invalid), scratch
  * An id outside 0..E-1 contributes nothing; an expert without
  * tokens is legal, and a token without any gets zeros.  Two runs give bit-identical results.
- * Limits: as the linear's for [F x H] and [H x F]; the codes of T rows of H and of T topk rows of F within 4 GiB each.
+ * Limits: as the linear's for [F x H] and [H x F]; T < 2^23, E max(H, F) <= 2^27; the codes of T rows of H and of T topk rows of
+ * F within 4 GiB each.  A routed pair's weighted output is kept in fp32 between the down projection and the sum over a token's pairs
+ * while all of them take at most 64 MiB so, else in the activations' type.
  * Errors: NULL, SHAPE (also unknown flags), WORKSPACE, ALIGN, HIP.
  */
 size_t milo_moe_w8a8_workspace(int64_t T, int64_t H, int64_t F, int E, int topk);

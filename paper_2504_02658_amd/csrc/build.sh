@@ -30,6 +30,7 @@ g++ -O2 -std=c++17 -fPIC -shared -D__HIP_PLATFORM_AMD__=1 -DUSE_ROCM=1 -D_GLIBCX
 hipcc $FLAGS -DMILO_FULL_WAITS -c gemm_tiled.hip -o _build/gemm_tiled_fw.o & pids+=($!)
 hipcc $FLAGS -DMILO_FULL_WAITS -c gemm_few.hip -o _build/gemm_few_fw.o & pids+=($!)
 hipcc $FLAGS $PRELOAD -DMILO_FULL_WAITS -c gemm_decode.hip -o _build/gemm_decode_fw.o & pids+=($!)
+hipcc $FLAGS -DMILO_FULL_WAITS -c w8_linear.hip -o _build/w8_linear_fw.o & pids+=($!)
 for p in "${pids[@]}"; do wait $p; done
 # The decode kernel counts outstanding memory operations by hand (see gemm_decode.hip): a streaming
 # wave requests in a fixed order (per chunk XC buffer-to-LDS copies of activations and per row block a
@@ -117,7 +118,7 @@ if bad or n == 0 or waits == 0:
 print("tiled kernel: no scratch access around %d hand-counted waits in %d variants" % (waits, n))
 PY
 hipcc --offload-arch=gfx950 -shared -fPIC -o "$OUT/libmilo.so" _build/pack.o _build/gemm_tiled.o _build/gemm_decode.o _build/gemm_few.o _build/gemm_mid.o _build/moe.o _build/api.o _build/gemm_static.o _build/compress.o _build/w8_linear.o _build/w8_wide.o _build/w8_moe.o _build/moe_route.o
-hipcc --offload-arch=gfx950 -shared -fPIC -o "$OUT/libmilo_fullwaits.so" _build/pack.o _build/gemm_tiled_fw.o _build/gemm_decode_fw.o _build/gemm_few_fw.o _build/gemm_mid.o _build/moe.o _build/api.o _build/gemm_static.o _build/compress.o _build/w8_linear.o _build/w8_wide.o _build/w8_moe.o _build/moe_route.o
+hipcc --offload-arch=gfx950 -shared -fPIC -o "$OUT/libmilo_fullwaits.so" _build/pack.o _build/gemm_tiled_fw.o _build/gemm_decode_fw.o _build/gemm_few_fw.o _build/gemm_mid.o _build/moe.o _build/api.o _build/gemm_static.o _build/compress.o _build/w8_linear_fw.o _build/w8_wide.o _build/w8_moe.o _build/moe_route.o
 # Every kernel the host code launches must have its launch stub in the library (a stub that the
 # compiler failed to emit only shows up as an undefined symbol when the library is loaded).
 for lib in libmilo.so libmilo_fullwaits.so; do

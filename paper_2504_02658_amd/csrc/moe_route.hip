@@ -253,6 +253,7 @@ static int launch_gate_tile(const GateArgs& a, hipStream_t stream) {
 }
 template <int IN>
 static int launch_gate(const GateArgs& a, hipStream_t stream) {
+    // Both sides at 64 experts of 2048: 1024 tokens 31.8 and 30.2 us, 512 18.2 and 30, 4096 103 and 32.
     if (a.T > 1024 && a.E <= kGateTileExperts) return a.E <= 16 ? launch_gate_tile<IN, 1>(a, stream) : launch_gate_tile<IN, 4>(a, stream);
     moe_gate_token_kernel<IN><<<dim3((unsigned)a.T), dim3(kGateThreads), 0, stream>>>(a);
     return launch_status();
@@ -265,7 +266,7 @@ using namespace milo;
 extern "C" int milo_moe_route(const milo_half* X, int64_t T, int64_t H, const milo_half* Wg, int E, int topk, int n_shared, unsigned flags,
                               int32_t* ids, float* gates, void* stream) {
     if (!X || !Wg || !ids || !gates) return MILO_ERR_NULL;
-    if (T < 1 || T > (int64_t(1) << 23) || H < 1 || H > (int64_t(1) << 20) || E < 1 || E > kRouteMaxExperts || topk < 1 || topk > E || topk > kRouteMaxTopk ||
+    if (T < 1 || T >= (int64_t(1) << 22) || H < 1 || H > (int64_t(1) << 20) || E < 1 || E > kRouteMaxExperts || topk < 1 || topk > E || topk > kRouteMaxTopk ||
         n_shared < 0 || n_shared > kRouteMaxTopk || (flags & ~(MILO_ACT_BF16 | MILO_ROUTE_RENORMALIZE)))
         return MILO_ERR_SHAPE;
     if (!aligned16(X) || !aligned16(Wg) || !aligned16(ids) || !aligned16(gates)) return MILO_ERR_ALIGN;

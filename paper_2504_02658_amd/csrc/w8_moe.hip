@@ -75,7 +75,9 @@ __device__ __forceinline__ int slot_of(const int32_t* s_ids, int topk, int t, in
 // fragment, and have the next run on its way.  No branch stands between the loads: what lies past an end is loaded from a
 // clamped place and multiplied with zeros.  STAGED: the codes of the rows fit LDS, and the workgroup forms them there (so the
 // layer takes two launches); else a launch of the row quantizer has formed them (every workgroup reads all of its rows, so the
-// saving grows with the tokens).
+// saving grows with the tokens).  Measured: 16 tokens to 8 experts of 14336 x 4096 read 940 MB in 167 us and 470 MB in 84 us, 5.6 TB/s;
+// one token to 8 of 1408 x 2048 46 MB in 12.8 us and 23 MB in 12.1 us, where the trips to memory one after another (ids, table,
+// activations, weights) count.
 constexpr int kFewUpRun = 2, kFewDownRun = 4;
 
 template <int IN, bool STAGED>
@@ -421,7 +423,8 @@ struct W8MoeLayout {
 static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8MoeLayout* L) {
     if (T < 1 || E < 1 || E > 65536 || topk < 1 || topk > E) return false;
     if (!w8_shape_ok(F, H) || !w8_shape_ok(H, F)) return false;
-    if (T > (int64_t(1) << 30) / topk) return false;
+    if (T >= (int64_t(1) << 23) || T > (int64_t(1) << 30) / topk) return false;
+    if (E > (int64_t(1) << 27) / (H > F ? H : F)) return false;         // (the grid's work items fit 32 bits)
     const int64_t P = T * topk, hb = w8_kblocks(H) * 64, fb = w8_kblocks(F) * 64;
     // rows of codes are addressed with 32-bit offsets
     if (T * hb >= 0xFFFF0000ll || P * fb >= 0xFFFF0000ll) return false;

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import oracle
-from tests.test_gpu_w8 import DTYPES, check_layer, check_linear, check_route, make_layer, normal, routing
+from test_gpu_w8 import DTYPES, check_layer, check_linear, check_route, make_layer, normal, routing
 
 pytestmark = pytest.mark.gpu
 
@@ -51,6 +51,26 @@ def test_linear_kernels(api, kernel, M, N, K, dtype):
     check_linear(Y, X, W)
 
 
+@pytest.mark.parametrize("kernel,M,N,K", [c for c in LINEARS if c[0].startswith("tile")])
+def test_tiles_count_their_waits(api, kernel, M, N, K):
+    # the library in which every hand-counted wait is a wait for everything agrees bit for bit
+    full = api.bind(api.FULLWAITS_LIB_PATH)
+    X, w = normal(M, (M, K), torch.float16).cuda(), api.pack_w8(normal(N, (N, K)).cuda())
+    Y = api.w8a8_gemm(X, w)
+    assert torch.equal(Y, api._native.w8_gemm(full.entries, X, w.w8, N, K, None, None)) and (Y != 0).any()
+
+
+@pytest.mark.parametrize("T,H,F", [(300, 128, 128), (500, 520, 1030), (260, 64, 4100)])
+def test_layer_tiles_count_their_waits(api, T, H, F):
+    full = api.bind(api.FULLWAITS_LIB_PATH)
+    layer, _ = make_layer(api, H, F, 3, seed=T)
+    X = normal(T, (T, H), torch.bfloat16).cuda()
+    ids, gates = (t.cuda() for t in routing(T, 3, 2, seed=T))
+    Y = layer.forward(X, ids, gates)
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    assert torch.equal(Y, api._native.w8_moe(full.entries, X, ids, gates, layer.table, H, F, 3, None, status, None)) and (Y != 0).any()
+
+
 def test_linear_kernels_are_all_here():
     assert {k for k, *_ in LINEARS} == set(KERNELS)
 
@@ -74,6 +94,19 @@ def test_layer_kernels(api, T, H, F, E, topk, dtype):
     X = normal(T, (T, H), dtype)
     ids, gates = routing(T, E, topk, seed=T * 7 + E)
     check_layer(layer.forward(X.cuda(), ids.cuda(), gates.cuda()), X, host, ids, gates)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,H,F,E,topk", [
+    (9, 2100, 300, 8, 2), (16, 1030, 1100, 64, 8), (2, 9000, 130, 3, 2), (5, 200, 14500, 4, 2), (15, 2176, 4400, 5, 1), (4, 4096, 256, 6, 2), (4, 4097, 256, 6, 2)])
+def test_layer_of_few_tokens_with_and_without_the_quantizer(api, T, H, F, E, topk, dtype):
+    # codes of X and of the SwiGLU rows that the products form themselves, or that a launch of the quantizer does (16 and 64 KB)
+    layer, host = make_layer(api, H, F, E, seed=T + H + F)
+    X = normal(T, (T, H), dtype)
+    ids, gates = routing(T, E, topk, seed=T * 5 + E)
+    ids[T - 1, 0] = E
+    check_layer(layer.forward(X.cuda(), ids.cuda(), gates.cuda()), X, host, ids, gates)
+    assert layer.routing_status() == 6
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

@@ -99,15 +99,16 @@ def test_sizes(L):
     assert L.milo_w8_packed_bytes(1, 1) == 16 * 128 + 64
     assert L.milo_w8_packed_bytes(17, 129) == 32 * 256 + 128
     assert L.milo_w8_packed_bytes(14336, 4096) == 14336 * 4096 + 14336 * 4
-    for N, K in ((0, 64), (64, 0), (-1, 64), (16, (1 << 17) + 1), ((1 << 23) + 1, 16)):
+    for N, K in ((0, 64), (64, 0), (-1, 64), (16, (1 << 17) + 1), (1 << 22, 16)):
         assert L.milo_w8_packed_bytes(N, K) == 0
     assert L.milo_w8a8_gemm_workspace(1, 64, 128) >= 16 * 128 + 64
     assert L.milo_w8a8_gemm_workspace(0, 64, 128) == 0 and L.milo_w8a8_gemm_workspace(4, 0, 128) == 0
-    assert L.milo_w8a8_gemm_workspace(1 << 24, 64, 128) == 0
+    assert L.milo_w8a8_gemm_workspace(1 << 22, 64, 128) == 0 and L.milo_w8a8_gemm_workspace((1 << 22) - 1, 64, 128) > 0
+    assert L.milo_w8a8_gemm_workspace(1 << 19, (1 << 17) + 1, 128) == 0 and L.milo_w8a8_gemm_workspace(1 << 19, 1 << 17, 128) > 0     # M N
     assert L.milo_moe_w8a8_workspace(4, 128, 256, 8, 2) > 0
     assert L.milo_moe_w8a8_workspace(512, 4096, 14336, 8, 2) >= 512 * 2 * 14336
     for bad in ((0, 128, 256, 8, 2), (4, 0, 256, 8, 2), (4, 128, 0, 8, 2), (4, 128, 256, 0, 1), (4, 128, 256, 8, 0), (4, 128, 256, 8, 9),
-                (1 << 23, 4096, 4096, 8, 2), (4, 128, 256, 65537, 2)):
+                (1 << 23, 4096, 4096, 8, 2), (1 << 23, 1, 1, 8, 1), (4, 128, 256, 65537, 2), (4, 64, 1 << 15, 1 << 13, 2)):
         assert L.milo_moe_w8a8_workspace(*bad) == 0
 
 
@@ -125,7 +126,7 @@ def test_pack_refuses(L):
 def test_linear_refuses(L):
     need = L.milo_w8a8_gemm_workspace(4, 32, 64)
     ok = [P, 4, 32, 64, P, 0, P, P, need, None]
-    for i, v, status in ((0, None, 1), (4, None, 1), (6, None, 1), (1, 0, 2), (1, (1 << 23) + 1, 2), (2, 0, 2), (3, -4, 2), (5, 1, 2), (5, 2, 2), (7, None, 5),
+    for i, v, status in ((0, None, 1), (4, None, 1), (6, None, 1), (1, 0, 2), (1, 1 << 22, 2), (2, 0, 2), (3, -4, 2), (5, 1, 2), (5, 2, 2), (7, None, 5),
                          (8, need - 1, 5), (0, ODD, 7), (4, ODD, 7), (6, ODD, 7), (7, ODD, 7)):
         a = list(ok)
         a[i] = v
@@ -134,7 +135,7 @@ def test_linear_refuses(L):
 
 def test_route_refuses(L):
     ok = [P, 4, 64, P, 8, 2, 1, 0, P, P, None]
-    for i, v, status in ((0, None, 1), (3, None, 1), (8, None, 1), (9, None, 1), (1, 0, 2), (2, 0, 2), (4, 0, 2), (4, 1025, 2), (5, 0, 2), (5, 9, 2), (6, -1, 2),
+    for i, v, status in ((0, None, 1), (3, None, 1), (8, None, 1), (9, None, 1), (1, 0, 2), (1, 1 << 22, 2), (2, 0, 2), (2, (1 << 20) + 1, 2), (4, 0, 2), (4, 1025, 2), (5, 0, 2), (5, 9, 2), (6, -1, 2),
                          (6, 65, 2), (7, 1, 2), (7, 16, 2), (0, ODD, 7), (3, ODD, 7), (8, ODD, 7), (9, ODD, 7)):
         a = list(ok)
         a[i] = v
