@@ -148,15 +148,31 @@ __device__ __forceinline__ void raw_values(const W8Raw<IN>& r, float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = raw_value<IN>(r, i);
 }
-// Largest magnitude so far, as fp32 bits.
+// Largest magnitude so far: of 16-bit elements in both halves of a word, as their bits without the sign (whose order is that of the
+// magnitudes, infinities and NaN on top), of fp32 as its bits.  top_bits() turns it into fp32 bits.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 template <int IN>
 __device__ __forceinline__ uint32_t raw_top(const W8Raw<IN>& r, uint32_t top) {
+    if constexpr (IN == W8_F32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t b = __float_as_uint(raw_value<IN>(r, i)) & 0x7fffffffu;
-        top = b > top ? b : top;
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t b = r.w[i] & 0x7fffffffu;
+            top = b > top ? b : top;
+        }
+        return top;
+    } else {
+        u16x2 t = __builtin_bit_cast(u16x2, top);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, r.w[i] & 0x7fff7fffu));
+        return __builtin_bit_cast(uint32_t, t);
     }
-    return top;
+}
+template <int IN>
+__device__ __forceinline__ uint32_t top_bits(uint32_t top) {
+    if constexpr (IN == W8_F32) return top;
+    const uint32_t lo = top & 0xffffu, hi = top >> 16, most = lo > hi ? lo : hi;
+    if constexpr (IN == W8_F16) return __float_as_uint((float)f16_bits(most)) & 0x7fffffffu;
+    else return most << 16;
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 #pragma unroll

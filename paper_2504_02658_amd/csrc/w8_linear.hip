@@ -20,8 +20,8 @@ static bool w8_linear_ok(int64_t M, int64_t N, int64_t K) { return w8_shape_ok(N
 // ---------------------------------------------------------------------------------------------
 // Row quantizer: a row is read once for its largest magnitude and, while it fits the registers of its TPR threads,
 // quantized from there.
-constexpr int kQuantHeld = 4;
-template <int IN, int TPR, int ROWS, bool BLOCKED>
+// (HELD: pieces of 16 that a thread holds.)
+template <int IN, int TPR, int ROWS, int HELD, bool BLOCKED>
 __global__ __launch_bounds__(TPR * ROWS) void w8_quant_kernel(const W8QuantArgs a, int kb) {
     constexpr int SZ = IN == W8_F32 ? 4 : 2;
     __shared__ uint32_t s_top[TPR * ROWS / 64];
@@ -31,17 +31,18 @@ __global__ __launch_bounds__(TPR * ROWS) void w8_quant_kernel(const W8QuantArgs 
     const char* in = reinterpret_cast<const char*>(a.in) + (there ? row : 0) * a.K * SZ;
     const int64_t K = there ? a.K : 0;          // (rows beyond the last are all zero)
     const int pieces = kb * 4;                  // of 16 columns, with the padding
-    W8Raw<IN> held[kQuantHeld];
+    W8Raw<IN> held[HELD];
     uint32_t top = 0u;
 #pragma unroll
-    for (int i = 0; i < kQuantHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
         const int p = tid + i * TPR;
-        held[i] = load16<IN>(in, (int64_t)p * 16, p < pieces ? K : 0);
+        held[i] = W8Raw<IN>{};
+        if (p < pieces) held[i] = load16<IN>(in, (int64_t)p * 16, K);
     }
 #pragma unroll
-    for (int i = 0; i < kQuantHeld; ++i) top = raw_top<IN>(held[i], top);
-    for (int p = tid + kQuantHeld * TPR; p < pieces; p += TPR) top = raw_top<IN>(load16<IN>(in, (int64_t)p * 16, K), top);
-    top = wave_max(top);
+    for (int i = 0; i < HELD; ++i) top = raw_top<IN>(held[i], top);
+    for (int p = tid + HELD * TPR; p < pieces; p += TPR) top = raw_top<IN>(load16<IN>(in, (int64_t)p * 16, K), top);
+    top = wave_max(top_bits<IN>(top));
     if constexpr (TPR > 64) {
         if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
         __syncthreads();
@@ -62,9 +63,9 @@ __global__ __launch_bounds__(TPR * ROWS) void w8_quant_kernel(const W8QuantArgs 
         *reinterpret_cast<u32x4*>(to) = c;
     };
 #pragma unroll
-    for (int i = 0; i < kQuantHeld; ++i)
+    for (int i = 0; i < HELD; ++i)
         if (tid + i * TPR < pieces) put(tid + i * TPR, held[i]);
-    for (int p = tid + kQuantHeld * TPR; p < pieces; p += TPR) put(p, load16<IN>(in, (int64_t)p * 16, K));
+    for (int p = tid + HELD * TPR; p < pieces; p += TPR) put(p, load16<IN>(in, (int64_t)p * 16, K));
     if (tid == 0) a.scales[row] = st.s;
 }
 
@@ -78,12 +79,13 @@ static int launch_quant(const W8QuantArgs& a, hipStream_t stream) {
     auto launch = [&](auto kernel, int threads, int per) { kernel<<<dim3((unsigned)((rows + per - 1) / per)), dim3(threads), 0, stream>>>(a, kb); };
     const int pieces = kb * 4;
     if (rows < 1024) {
-        if (pieces <= 256) launch(w8_quant_kernel<IN, 256, 1, BLOCKED>, 256, 1);
-        else launch(w8_quant_kernel<IN, 1024, 1, BLOCKED>, 1024, 1);
+        if (pieces <= 256) launch(w8_quant_kernel<IN, 256, 1, 1, BLOCKED>, 256, 1);
+        else if (pieces <= 1024) launch(w8_quant_kernel<IN, 1024, 1, 1, BLOCKED>, 1024, 1);
+        else launch(w8_quant_kernel<IN, 1024, 1, 4, BLOCKED>, 1024, 1);
     } else {
-        if (pieces <= 64 * kQuantHeld) launch(w8_quant_kernel<IN, 64, 16, BLOCKED>, 1024, 16);
-        else if (pieces <= 256 * kQuantHeld) launch(w8_quant_kernel<IN, 256, 4, BLOCKED>, 1024, 4);
-        else launch(w8_quant_kernel<IN, 1024, 1, BLOCKED>, 1024, 1);
+        if (pieces <= 256) launch(w8_quant_kernel<IN, 64, 16, 4, BLOCKED>, 1024, 16);
+        else if (pieces <= 1024) launch(w8_quant_kernel<IN, 256, 4, 4, BLOCKED>, 1024, 4);
+        else launch(w8_quant_kernel<IN, 1024, 1, 4, BLOCKED>, 1024, 1);
     }
     return launch_status();
 }

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8Few
             if (s_slot[t] < 0) continue;
             uint32_t top = 0u;
             for (int p = tid; p < pieces; p += kFewUpThreads) top = raw_top<IN>(load16<IN>(X + t * a.H * 2, (int64_t)p * 16, a.H), top);
-            top = wave_max(top);
+            top = wave_max(top_bits<IN>(top));
             if (lane == 0) s_top[t][wave] = top;
         }
         __syncthreads();

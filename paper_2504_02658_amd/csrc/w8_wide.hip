@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
         for (int m = wave / share; m < rows; m += NW / share) {
             uint32_t top = 0u;
             for (int p = part * 64 + lane; p < pieces; p += share * 64) top = raw_top<IN>(load16<IN>(X + m * a.K * 2, (int64_t)p * 16, a.K), top);
-            top = wave_max(top);
+            top = wave_max(top_bits<IN>(top));
             if (lane == 0) s_top[m][part] = top;
         }
         __syncthreads();
