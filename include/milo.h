@@ -381,7 +381,7 @@ int milo_moe_w3lr_routing_status(const void* workspace, void* stream);
  * with the sum exact in 32-bit integers (whatever the order), its products with the scales in fp32 and one rounding to
  * the output type.  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale
  * NaN, so that what is computed from it is NaN and nothing else is touched.
- * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M < 2^22, N K, M K <= 2^40 and M N <= 2^36; nothing has to
+ * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M < 2^22, N K, M K and M N <= 2^36; nothing has to
  * be a multiple of anything.  Pointers are 16-byte aligned, arrays dense.  These calls need no prepared workspace: theirs is scratch
  * alone, may hold anything before and after, and keeps nothing between calls; no kernel of theirs waits for another workgroup,
  * so that they run beside other streams' work and can be captured in a graph.

@@ -11,8 +11,9 @@ namespace milo {
 // A row's sums have to fit 32 bits: 127 * 127 * K < 2^31.
 constexpr int64_t kW8MaxK = 1 << 17;
 
+// (and the quantizer's grid of up to 1024 threads per row fits 32 bits of work items: 2^22 rows go with K <= 16384, where it takes 256)
 bool w8_shape_ok(int64_t N, int64_t K) {
-    return N >= 1 && K >= 1 && K <= kW8MaxK && N < (int64_t(1) << 22) && N <= (int64_t(1) << 40) / K;
+    return N >= 1 && K >= 1 && K <= kW8MaxK && N < (int64_t(1) << 22) && N <= (int64_t(1) << 36) / K;
 }
 // (and a grid's work items fit 32 bits: one per 16 outputs with the smallest tiles that large products take)
 static bool w8_linear_ok(int64_t M, int64_t N, int64_t K) { return w8_shape_ok(N, K) && w8_shape_ok(M, K) && M <= (int64_t(1) << 36) / N; }

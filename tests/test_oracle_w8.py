@@ -94,6 +94,13 @@ def L():
     return api.lib()
 
 
+def test_sizes_whose_grids_fit(L):
+    # 2^36 numbers at most: padded to 2^22 rows, more of them would need 2^32 threads of the quantizer
+    for N, K in (((1 << 22) - 1, 1 << 14), (1 << 19, 1 << 17)):
+        assert L.milo_w8_packed_bytes(N, K) > 0 and L.milo_w8a8_gemm_workspace(N, 1, K) > 0
+        assert L.milo_w8_packed_bytes(N, K + 1) == 0 and L.milo_w8a8_gemm_workspace(N, 1, K + 1) == 0
+
+
 def test_sizes(L):
     assert L.milo_w8_packed_bytes(16, 128) == 16 * 128 + 64
     assert L.milo_w8_packed_bytes(1, 1) == 16 * 128 + 64
