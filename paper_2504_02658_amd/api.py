@@ -435,6 +435,8 @@ class W8MoELayer:
         for e, (w1, w3, w2) in enumerate(experts):
             if (w1.N, w1.K, w3.N, w3.K, w2.N, w2.K) != (self.F, self.H, self.F, self.H, self.H, self.F):
                 raise ValueError(f"expert {e}: w1 and w3 must be [F, H], w2 [H, F]")
+            if any(w.w8.dtype != torch.uint8 or not w.w8.is_contiguous() or w.w8.numel() < lib().milo_w8_packed_bytes(w.N, w.K) for w in (w1, w3, w2)):
+                raise ValueError(f"expert {e}: a packed weight is smaller than its shape says")
             arr[e] = W8Expert(w1.w8.data_ptr(), w3.w8.data_ptr(), w2.w8.data_ptr())
         _check(lib().milo_moe_w8a8_check_experts(arr, self.E, self.H, self.F), "milo_moe_w8a8_check_experts")
         device = experts[0][0].w8.device

@@ -1,11 +1,12 @@
 // milo_moe_w8a8_forward: top-k routed SwiGLU experts over 8-bit integer linears.
 //
-// Up to kFewTokens tokens, two launches, both bound by the bytes of the weights of the experts that some token goes to:
+// Up to kFewTokens tokens, two products, both bound by the bytes of the weights of the experts that some token goes to:
 //   few_up    a workgroup owns 16 of the F features of one expert (gate and up): it finds the expert's tokens in the ids,
-//             quantizes their activations, multiplies, and writes H = SiLU(gate) * up with the largest magnitude of
-//             its 16 features per row
-//   few_down  a workgroup owns 16 of the H features of the output and walks all experts: it quantizes the rows of H and
-//             adds each expert's product, weighted, to the tokens' sums, so that nothing is left to combine
+//             multiplies their codes, and writes H = SiLU(gate) * up with the largest magnitude of its 16 features per row
+//   few_down  a workgroup owns 16 of the H features of the output and walks all experts: it adds each expert's product,
+//             weighted, to the tokens' sums, so that nothing is left to combine
+// Either quantizes its rows itself while their codes are few (kFewUpStaged, kFewDownStaged), else a launch of the row quantizer goes
+// in front of it: two to four launches.
 // More tokens: the activations' rows are quantized once, pairs grouped per expert (route_kernel of moe.hip), gate and up as one
 // grouped product over the tiles, the SwiGLU rows quantized, the grouped down projection, and the sum over a token's pairs.
 #include "milo_host.h"
@@ -303,9 +304,9 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
     auto work = [&](int r, int from) {
         const int s = r / runs, u = (r - s * runs) * B;
         const float f = s_factor[s][m];
+        const int row = s_row[s][m];
         const f32x4 sw = *reinterpret_cast<const f32x4*>(&s_sw[s][c16 * 4]);
         if constexpr (STAGED) {
-            const int row = s_row[s][m];
 #pragma unroll
             for (int i = 0; i < B; ++i) {
                 q[from][i] = *reinterpret_cast<const u32x4*>(codes + (((u + i < kb ? u + i : 0) * 4 + c16) * P + (row >= 0 ? row : 0)) * 16);
@@ -319,7 +320,7 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
 #pragma unroll
         for (int i = 0; i < B; ++i) acc = mfma16_i8(w[from][i], q[from][i], acc);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += (float)acc[i] * f * sw[i];
+        for (int i = 0; i < 4; ++i) y[i] += row >= 0 ? (float)acc[i] * f * sw[i] : 0.0f;      // (another token's expert may have a scale that is no number)
     };
     for (int r = wave; r < all; r += 2 * NW) {
         work(r, 0);

@@ -349,6 +349,29 @@ def test_layer_special_tokens(api, T):
     assert torch.equal(Y[3:], want[3:])
 
 
+@pytest.mark.parametrize("T,F", [(3, 150), (16, 2200), (50, 150)])
+def test_layer_expert_that_is_no_number(api, T, F):
+    # NaN and infinities in one expert's weights reach its own tokens alone
+    H, E = 200, 4
+    X = normal(T, (T, H), torch.float16)
+    ids, gates = routing(T, E, 2, seed=T)
+    ids[:, 0], ids[:, 1] = 0, 1
+    ids[0, 1], ids[1, 0] = 2, 3
+    W = [[normal(80 + 3 * e + i, s, torch.float16, 0.05) for i, s in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+
+    def run():
+        layer = api.W8MoELayer([tuple(api.pack_w8(w.cuda()) for w in ws) for ws in W], H, F)
+        return layer.forward(X.cuda(), ids.cuda(), gates.cuda()).cpu()
+
+    want = run()
+    W[2][2][5, 7] = float("nan")        # one output of token 0
+    W[3][0][F - 1, 0] = float("inf")    # all of token 1, whose row of F has a NaN
+    Y = run()
+    assert torch.isnan(Y[0, 5]) and torch.isnan(Y[1]).all()
+    want[0, 5] = Y[0, 5] = 0.0
+    assert torch.equal(Y[0], want[0]) and torch.equal(Y[2:], want[2:])
+
+
 @pytest.mark.parametrize("T,topk", [(1, 3), (9, 2), (33, 2), (400, 2)])
 def test_layer_runs_agree_and_leave_neighbours(api, T, topk):
     H, F, E = 264, 200, 6
@@ -387,6 +410,9 @@ def test_layer_refuses(api):
     w = api.pack_w8(normal(1, (96, 64)).cuda())
     with pytest.raises(ValueError):
         api.W8MoELayer([(w, w, w)], 64, 96)
+    short, down = api.W8Weight(96, 64, w.w8[:-16]), api.pack_w8(normal(2, (64, 96)).cuda())
+    with pytest.raises(ValueError):
+        api.W8MoELayer([(w, short, down)], 64, 96)
 
 
 # ---- together ----------------------------------------------------------------------------------------------
