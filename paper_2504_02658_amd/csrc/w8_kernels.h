@@ -35,6 +35,7 @@ struct W8TileArgs {
     const milo_w8_expert* experts;  // EPI 1, 2: device table
     const TileDesc* tiles;
     int m_tiles, n_tiles;           // EPI 1, 2: m_tiles slots, some of them empty; the rest is set at the launch
+    int group_m, span;              // order of the tiles (below)
     const int32_t* x_rows;          // EPI 1: token of a sorted row;  EPI 2: pair of a sorted row
     const float* gates;             // EPI 2: factor per pair
     void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N], the activations' type with out16, else fp32
@@ -54,16 +55,17 @@ int launch_w8_wide(const W8TileArgs& a, int epi, int tm, int rn, hipStream_t str
 
 
 // Tile of a workgroup.  Workgroup i runs on XCD i % 8, each of which has an L2 of its own, so every XCD gets a contiguous range of
-// an order in which tiles that share rows or columns are close: groups of kW8GroupM tiles of rows, and inside a group all columns,
-// rows fastest.
-constexpr int kW8GroupM = 8;
-__device__ __forceinline__ void w8_tile_of(uint32_t i, int m_tiles, int n_tiles, int* mt, int* nt) {
+// an order in which tiles that share rows or columns are close: groups of group_m tiles of rows; inside a group runs of `span` columns;
+// inside a run one tile of rows after the other.
+__device__ __forceinline__ void w8_tile_of(uint32_t i, int m_tiles, int n_tiles, int group_m, int span, int* mt, int* nt) {
     const uint32_t total = (uint32_t)m_tiles * (uint32_t)n_tiles, x = i & 7u, per = total >> 3, rem = total & 7u;
     const uint32_t l = x * per + (x < rem ? x : rem) + (i >> 3);
-    const uint32_t group = l / (uint32_t)(kW8GroupM * n_tiles), in = l - group * (uint32_t)(kW8GroupM * n_tiles);
-    const uint32_t left = (uint32_t)m_tiles - group * kW8GroupM, rows = left < kW8GroupM ? left : kW8GroupM;
-    *nt = (int)(in / rows);
-    *mt = (int)(group * kW8GroupM + in % rows);
+    const uint32_t group = l / (uint32_t)(group_m * n_tiles), in = l - group * (uint32_t)(group_m * n_tiles);
+    const uint32_t left = (uint32_t)m_tiles - group * (uint32_t)group_m, rows = left < (uint32_t)group_m ? left : (uint32_t)group_m;
+    const uint32_t run = in / (rows * (uint32_t)span), at = in - run * rows * (uint32_t)span, n0 = run * (uint32_t)span;
+    const uint32_t cols = (uint32_t)n_tiles - n0 < (uint32_t)span ? (uint32_t)n_tiles - n0 : (uint32_t)span, r = at / cols;
+    *nt = (int)(n0 + at - r * cols);
+    *mt = (int)(group * (uint32_t)group_m + r);
 }
 
 

@@ -103,9 +103,8 @@ int launch_w8_quant(const W8QuantArgs& a, int in, hipStream_t stream) {
 
 // The tiled product.  WM x WN waves (times WK, which share K), each with TM x TN tiles of 32 x 32; NS stages of 64 columns in LDS.
 // Copies go from memory to LDS directly, as the operands are stored.  What a stage of the widest tile costs: 16 KB + 8 KB from the L2,
-// 8 matrix instructions of 32 cycles per wave, two of its workgroups per compute unit.  4096 x 4096 x 14336: 214 us on a cool card with the matrix
-// cores busy 60 % of the cycles, 258 back to back, where the loop without copies and LDS reads takes 200: the clock falls under this
-// load.  Small tiles are bound by the L2 (about 11 to 14 TB/s into LDS in all), so the widest that fills the chip is taken.
+// 8 matrix instructions of 32 cycles per wave, two of its workgroups per compute unit.  4096 x 4096 x 14336: 213 us on a cool card with the matrix
+// cores busy 70 % of the cycles at 1.55 GHz, 236 back to back: the clock falls under this load.  Small tiles are bound by the L2 (about 11 to 14 TB/s into LDS in all), so the widest that fills the chip is taken.
 template <int WM, int WN, int WK, int TM, int TN, int NS, int EPI, bool BF>
 __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8TileArgs a) {
     constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
     const int wk = wave_all / NW, wave = wave_all - wk * NW;
     const int kb = (int)w8_kblocks(a.K), stages = kb / WK;
     int mt, nt;
-    w8_tile_of(blockIdx.x, a.m_tiles, a.n_tiles, &mt, &nt);
+    w8_tile_of(blockIdx.x, a.m_tiles, a.n_tiles, a.group_m, a.span, &mt, &nt);
     const int64_t n0 = (int64_t)nt * OUTN;
     int64_t row0;
     int rows;
@@ -140,6 +139,9 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
         w0 = reinterpret_cast<const uint8_t*>(EPI == 1 ? e.w1 : e.w2);
         w1 = reinterpret_cast<const uint8_t*>(EPI == 1 ? e.w3 : e.w2);
     }
+    // EPI 1, 2: four neighbouring lanes copy the 64 bytes of one row, so that they make one request (a lane per row, in the blocks' order, makes four: 512
+    // tokens of 8 experts of 14336 x 4096 497 us against 483).  Then rows are 64 bytes apart in LDS, and of 16 rows that are read at once
+    // four would meet in the same banks: piece p of row r is put at p ^ (r / 4 % 4).
     // where this wave's copies come from: activations, then the weight (gate and up: half of the rows each)
     const uint64_t wbytes = (uint64_t)w8_code_bytes(a.N, a.K), wskip = (uint64_t)(n0 >> 4) * kb * 1024;
     const uint64_t abase = EPI == 0 ? (uint64_t)row0 / 16 * kb * 1024 : 0;
@@ -152,10 +154,10 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
         if constexpr (EPI == 0) {
             aoff[i] = (uint32_t)(b * kb + wk) * 1024u + lane * 16;
         } else {
-            int r = b * 16 + (lane & 15);
+            int r = b * 16 + (lane >> 2);
             r = (int)row0 + (r < rows ? r : 0);         // (rows beyond the tile's: computed, not stored)
             const int64_t src = EPI == 1 ? a.x_rows[r] : r;
-            aoff[i] = (uint32_t)(src * kb * 64) + wk * 64 + (lane >> 4) * 16;
+            aoff[i] = (uint32_t)(src * kb * 64) + wk * 64 + ((lane ^ lane >> 4) & 3) * 16;
         }
     }
 #pragma unroll
@@ -178,6 +180,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
     };
     const int wm = wave % WM, wn = wave / WM, l32 = lane & 31, h = lane >> 5;
     const int frag = (l32 >> 4) * 1024 + h * 256 + (l32 & 15) * 16;
+    const int afrag = EPI == 0 ? frag : (l32 >> 4) * 1024 + (l32 & 15) * 64 + ((h ^ l32 >> 2) & 3) * 16;
     // The wave's m-th block of 32 rows is block m * WM + wm of the tile; blocks past the tile's rows take no part (the loop is there
     // once for every number of blocks, and its body has no branches).
     const int blocks = (rows + 31) / 32, used = (blocks - wm + WM - 1) / WM;
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
         constexpr int MBU = decltype(mbu)::value;
         u32x4 af[2][MBU > 0 ? MBU : 1], bf[2][TN];
         auto read = [&](int c, int k) {
-            const unsigned char* const as = smem + (c % NS) * STAGE + wk * PART + wm * 2048 + frag + k * 512;
+            const unsigned char* const as = smem + (c % NS) * STAGE + wk * PART + wm * 2048 + (EPI == 0 ? frag + k * 512 : afrag ^ k * 32);
             const unsigned char* const bs = smem + (c % NS) * STAGE + wk * PART + ABLK * 1024 + frag + k * 512;
             if constexpr (MBU > 0) {
 #pragma unroll
@@ -495,6 +498,8 @@ extern "C" int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t 
     a.N = N;
     a.K = K;
     a.w = w8;
+    a.group_m = 8;
+    a.span = 1;
     a.out = Y;
     a.act_bf16 = bf;
     if (M <= 16 && M * w8_kblocks(K) * 64 <= kW8WideStaged) {

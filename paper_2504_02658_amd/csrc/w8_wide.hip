@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kWideWaves * 64, 2) void w8_wide_kernel(const W8Til
     const int m16 = lane & 15, c16 = lane >> 4;
     const int kb = (int)w8_kblocks(a.K);
     int mt, nt;
-    w8_tile_of(blockIdx.x, a.m_tiles, a.n_tiles, &mt, &nt);
+    w8_tile_of(blockIdx.x, a.m_tiles, a.n_tiles, a.group_m, a.span, &mt, &nt);
     const int64_t n0 = (int64_t)nt * OUTN;
     int64_t row0;
     int rows;
