@@ -60,7 +60,7 @@ def test_tiles_count_their_waits(api, kernel, M, N, K):
     assert torch.equal(Y, api._native.w8_gemm(full.entries, X, w.w8, N, K, None, None)) and (Y != 0).any()
 
 
-@pytest.mark.parametrize("T,H,F", [(300, 128, 128), (500, 520, 1030), (260, 64, 4100)])
+@pytest.mark.parametrize("T,H,F", [(300, 128, 128), (500, 520, 1030), (260, 64, 4100), (300, 5000, 130), (260, 4500, 1030)])
 def test_layer_tiles_count_their_waits(api, T, H, F):
     full = api.bind(api.FULLWAITS_LIB_PATH)
     layer, _ = make_layer(api, H, F, 3, seed=T)
@@ -88,7 +88,8 @@ def test_rows_quantized_at_every_width(api, M, K):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("T,H,F,E,topk", [
     (300, 128, 128, 4, 2), (300, 130, 129, 4, 2), (260, 96, 500, 3, 1), (257, 520, 131, 2, 2), (900, 64, 258, 3, 3), (150, 72, 14400, 2, 1), (129, 40, 3, 1, 1),
-    (100, 4096, 257, 16, 2), (17, 300, 520, 64, 8), (40, 513, 130, 30, 3)])
+    (100, 4096, 257, 16, 2), (17, 300, 520, 64, 8), (40, 513, 130, 30, 3),
+    (300, 5000, 130, 3, 2), (260, 4502, 1030, 3, 2)])       # (tiles of 256 features in the down product: more than 128 of them)
 def test_layer_kernels(api, T, H, F, E, topk, dtype):
     layer, host = make_layer(api, H, F, E, seed=T + H + F)
     X = normal(T, (T, H), dtype)
