@@ -444,9 +444,10 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         return at;
     };
     L->few = T <= kFewTokens && P <= kFewMaxPairs;
-    // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest (66 experts of
-    // 1408 x 2048, 64 tokens: 149 us against 168 with tiles of 128 x 256; 8 experts of 14336 x 4096, 64 tokens: 331 against 300).
-    L->kernel = P < 12 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
+    // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest.  In those and in tiles of
+    // 128 x 256, us: 8 experts of 14336 x 4096, 10 rows each 260 and 293, 16 rows 268 and 296, 24 rows 288 and 305; 66 of 1408 x 2048, 8 rows 135 and
+    // 143, 19 rows 151 and 153, 31 rows 169 and 161.
+    L->kernel = P < 24 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
     L->off_h = take((size_t)P * F * 4);
     L->off_xq = take((size_t)(T * hb));
     L->off_xs = take((size_t)T * 4);
