@@ -451,8 +451,7 @@ int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H,
  * An id outside 0..E-1 contributes nothing; an expert without
  * tokens is legal, and a token without any gets zeros.  Two runs give bit-identical results.
  * Limits: as the linear's for [F x H] and [H x F]; T < 2^23, E max(H, F) <= 2^27; the codes of T rows of H and of T topk rows of
- * F within 4 GiB each.  A routed pair's weighted output is kept in fp32 between the down projection and the sum over a token's pairs
- * while all of them take at most 64 MiB so, else in the activations' type.
+ * F within 4 GiB each.  A routed pair's weighted output stays fp32 until it is added to its token's sum, whose rounding to the output type is the only one.
  * Errors: NULL, SHAPE (also unknown flags), WORKSPACE, ALIGN, HIP.
  */
 size_t milo_moe_w8a8_workspace(int64_t T, int64_t H, int64_t F, int E, int topk);

@@ -38,9 +38,8 @@ struct W8TileArgs {
     int group_m, span;              // order of the tiles (below)
     const int32_t* x_rows;          // EPI 1: token of a sorted row;  EPI 2: pair of a sorted row
     const float* gates;             // EPI 2: factor per pair
-    void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N], the activations' type with out16, else fp32
-    int out16;
-    int act_bf16;
+    void* out;                      // EPI 0: [M x N] 16-bit;  EPI 1: [rows x N] fp32;  EPI 2: [pairs x N] fp32
+    int act_bf16;                   // EPI 0
 };
 // The kernels of a product, named by rows x features of a workgroup (EPI 1: half as many output features, from gate and up).
 enum W8Kernel { W8_WIDE_16x16, W8_WIDE_16x32, W8_WIDE_16x64, W8_WIDE_32x32, W8_WIDE_32x64, W8_WIDE_64x64, W8_TILE_64x128, W8_TILE_128x128, W8_TILE_128x256 };

@@ -287,85 +287,82 @@ __global__ __launch_bounds__(WM * WN * WK * 64, 2) void w8_tile_kernel(const W8T
     const auto sw0 = global_float(w8_scales(w0, a.N, a.K)), sw1 = global_float(w8_scales(w1, a.N, a.K));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    auto each = [&](auto&& put) {       // put(row of the tile, column of the tile, four values)
+    // of the wave's m-th block: put(row of the tile, column of the tile, four values)
+    auto block = [&](int m, auto&& put) {
+        const int r = (m * WM + wm) * 32 + l32;
+        if (r >= rows || wk != 0) return;           // (with K in two halves, the first one's waves have the sums)
+        const int64_t row = row0 + r;
+        float sx;
+        if constexpr (EPI == 0) sx = a.a_scales[row];
+        else if constexpr (EPI == 1) sx = a.a_scales[a.x_rows[row]];
+        else sx = a.a_scales[row] * a.gates[a.x_rows[row]];
 #pragma unroll
-        for (int m = 0; m < TM; ++m) {
-            const int r = (m * WM + wm) * 32 + l32;
-            if (r >= rows || wk != 0) continue;         // (with K in two halves, the first one's waves have the sums)
-            const int64_t row = row0 + r;
-            float sx;
-            if constexpr (EPI == 0) sx = a.a_scales[row];
-            else if constexpr (EPI == 1) sx = a.a_scales[a.x_rows[row]];
-            else sx = a.a_scales[row] * a.gates[a.x_rows[row]];
+        for (int n = 0; n < (EPI == 1 ? TN / 2 : TN); ++n)
 #pragma unroll
-            for (int n = 0; n < (EPI == 1 ? TN / 2 : TN); ++n)
+            for (int i = 0; i < 4; ++i) {
+                const int c = (EPI == 1 ? wn * (TN / 2) + n : wn * TN + n) * 32 + 8 * i + 4 * h;
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (n0 + c < a.N) {         // (there are scales for whole blocks of 16)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = (EPI == 1 ? wn * (TN / 2) + n : wn * TN + n) * 32 + 8 * i + 4 * h;
-                    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (n0 + c < a.N) {         // (there are scales for whole blocks of 16)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            v[j] = (float)acc[n][m][4 * i + j] * sx * sw0[n0 + c + j];
-                            if constexpr (EPI == 1) v[j] = silu_times(v[j], (float)acc[n + TN / 2][m][4 * i + j] * sx * sw1[n0 + c + j]);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        v[j] = (float)acc[n][m][4 * i + j] * sx * sw0[n0 + c + j];
+                        if constexpr (EPI == 1) v[j] = silu_times(v[j], (float)acc[n + TN / 2][m][4 * i + j] * sx * sw1[n0 + c + j]);
                     }
-                    put(r, c, v);
                 }
-        }
+                put(r, c, v);
+            }
+    };
+    auto each = [&](auto&& put) {
+#pragma unroll
+        for (int m = 0; m < TM; ++m) block(m, put);
     };
     constexpr int threads = WM * WN * WK * 64;
     const int tid = threadIdx.x;
-    if constexpr (EPI == 1) {
-        // fp32: the quantizer that follows has to see the value that it rounds.  (16-bit fixed point with a scale per row and 128 features moves
-        // one code in 600, and one step of a code in 600 is 0.16 % of the layer's output, eight times what fp16 rounds off; it took 35 us
-        // less of 540, 4096 tokens of 66 experts of 1408.)
+    if constexpr (EPI != 0) {
+        // fp32.  SwiGLU rows: the quantizer that follows has to see the value that it rounds.  (16-bit fixed point with a scale per row and 128
+        // features moves one code in 600, and one step of a code in 600 is 0.16 % of the layer's output, eight times what fp16 rounds off; it took
+        // 35 us less of 540, 4096 tokens of 66 experts of 1408.)  A pair's weighted output: the sum over a token's pairs may cancel, and may
+        // fit 16 bits where a term does not.  The room is that of all rows of half as many columns (gate and up), or of WM blocks of rows.
         float* const tile = reinterpret_cast<float*>(smem);
-        constexpr int PITCH = OUTN + 4, Q = OUTN / 4;
-        static_assert(BM * PITCH * 4 <= NS * STAGE, "room for the tile");
-        each([&](int r, int c, const float (&v)[4]) { *reinterpret_cast<f32x4*>(tile + r * PITCH + c) = f32x4{v[0], v[1], v[2], v[3]}; });
-        __syncthreads();
-        for (int r = tid / Q; r < rows; r += threads / Q) {
-            const int c = (tid % Q) * 4;
-            const f32x4 v = *reinterpret_cast<const f32x4*>(tile + r * PITCH + c);
-            float* const to = reinterpret_cast<float*>(a.out) + (row0 + r) * a.N + n0 + c;
-            if ((a.N & 3) == 0) {
-                if (n0 + c < a.N) *reinterpret_cast<f32x4*>(to) = v;
-            } else {
+        constexpr int PITCH = OUTN + 4, Q = OUTN / 4, PARTS = EPI == 1 ? 1 : TM, ROWS = BM / PARTS;
+        static_assert(ROWS * PITCH * 4 <= NS * STAGE, "room for a part of the tile");
+        auto put = [&](int r, int c, const float (&v)[4]) { *reinterpret_cast<f32x4*>(tile + (r % ROWS) * PITCH + c) = f32x4{v[0], v[1], v[2], v[3]}; };
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (n0 + c + j < a.N) to[j] = v[j];
+        for (int part = 0; part < PARTS; ++part) {
+            if (part > 0) __syncthreads();              // (the part before has left)
+            if constexpr (PARTS == 1) each(put);
+            else block(part, put);
+            __syncthreads();
+            for (int r = part * ROWS + tid / Q; r < rows && r < (part + 1) * ROWS; r += threads / Q) {
+                const int c = (tid % Q) * 4;
+                const f32x4 v = *reinterpret_cast<const f32x4*>(tile + (r % ROWS) * PITCH + c);
+                float* const to = reinterpret_cast<float*>(a.out) + (EPI == 1 ? row0 + r : (int64_t)a.x_rows[row0 + r]) * a.N + n0 + c;
+                if ((a.N & 3) == 0) {
+                    if (n0 + c < a.N) *reinterpret_cast<f32x4*>(to) = v;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (n0 + c + j < a.N) to[j] = v[j];
+                }
             }
         }
+    } else if ((a.N & 7) != 0) {
+        const bool vec = (a.N & 3) == 0;
+        each([&](int r, int c, const float (&v)[4]) {
+            const int64_t col = n0 + c;
+            if (col >= a.N) return;
+            store4<BF>(reinterpret_cast<uint16_t*>(a.out) + (row0 + r) * a.N + col, v, (int)(a.N - col < 4 ? a.N - col : 4), vec);
+        });
     } else {
-        const bool out32 = EPI == 2 && !a.out16;
-        if (out32 || (a.N & 7) != 0) {
-            const bool vec = (a.N & 3) == 0;
-            each([&](int r, int c, const float (&v)[4]) {
-                const int64_t col = n0 + c, to = EPI == 2 ? a.x_rows[row0 + r] : row0 + r;
-                if (col >= a.N) return;
-                const int left = (int)(a.N - col < 4 ? a.N - col : 4);
-                if (!out32) {
-                    store4<BF>(reinterpret_cast<uint16_t*>(a.out) + to * a.N + col, v, left, vec);
-                } else {
-                    float* const o = reinterpret_cast<float*>(a.out) + to * a.N + col;
-                    if (vec) *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-                    else
-                        for (int j = 0; j < left; ++j) o[j] = v[j];
-                }
-            });
-        } else {
-            uint16_t* const tile = reinterpret_cast<uint16_t*>(smem);
-            constexpr int PITCH = BN + 8;
-            static_assert(BM * PITCH * 2 <= NS * STAGE, "room for the tile");
-            each([&](int r, int c, const float (&v)[4]) { store4<BF>(tile + r * PITCH + c, v, 4, true); });
-            __syncthreads();
-            for (int r = tid / (BN / 8); r < rows; r += threads / (BN / 8)) {
-                const int c = (tid % (BN / 8)) * 8;
-                if (n0 + c >= a.N) continue;
-                const int64_t to = EPI == 2 ? a.x_rows[row0 + r] : row0 + r;
-                *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.out) + to * a.N + n0 + c) = *reinterpret_cast<const u32x4*>(tile + r * PITCH + c);
-            }
+        uint16_t* const tile = reinterpret_cast<uint16_t*>(smem);
+        constexpr int PITCH = BN + 8;
+        static_assert(BM * PITCH * 2 <= NS * STAGE, "room for the tile");
+        each([&](int r, int c, const float (&v)[4]) { store4<BF>(tile + r * PITCH + c, v, 4, true); });
+        __syncthreads();
+        for (int r = tid / (BN / 8); r < rows; r += threads / (BN / 8)) {
+            const int c = (tid % (BN / 8)) * 8;
+            if (n0 + c >= a.N) continue;
+            *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.out) + (row0 + r) * a.N + n0 + c) = *reinterpret_cast<const u32x4*>(tile + r * PITCH + c);
         }
     }
 }
@@ -399,8 +396,8 @@ static int launch_w8_tile(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t 
     // Tiles that are half as wide where the wide ones would leave half of the compute units without one (45 tokens of 17 experts of 2730 x 1000: 49.6 us
     // against 54.4 for the layer; where they fill the chip they cost more: 512 tokens of 8 of 14336 x 4096 473 against 448).
     if ((int64_t)a.m_tiles * ((a.N + 255) / 256) <= device_cus() / 2)
-        return a.act_bf16 ? launch_tile<2, 4, 1, 2, 1, 4, 2, true>(a, stream) : launch_tile<2, 4, 1, 2, 1, 4, 2, false>(a, stream);
-    return a.act_bf16 ? launch_tile<2, 4, 1, 2, 2, 3, 2, true>(a, stream) : launch_tile<2, 4, 1, 2, 2, 3, 2, false>(a, stream);
+        return launch_tile<2, 4, 1, 2, 1, 4, 2, false>(a, stream);
+    return launch_tile<2, 4, 1, 2, 2, 3, 2, false>(a, stream);
 }
 int w8_kernel_rows(W8Kernel k) {
     switch (k) {

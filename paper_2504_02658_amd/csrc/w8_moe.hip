@@ -381,10 +381,9 @@ static int launch_few(const W8FewArgs& a, hipStream_t s) {
 
 // ---------------------------------------------------------------------------------------------
 // Y = sum over a token's pairs of their rows of O, in slot order; a pair whose id is out of range has none.
-template <bool BF, bool OUT16>
-__global__ __launch_bounds__(256) void w8_combine_kernel(const void* __restrict__ O, const int32_t* __restrict__ ids, int topk, int E, int64_t H,
+template <bool BF>
+__global__ __launch_bounds__(256) void w8_combine_kernel(const float* __restrict__ O, const int32_t* __restrict__ ids, int topk, int E, int64_t H,
                                                          uint16_t* __restrict__ Y) {
-    constexpr int IN = OUT16 ? (BF ? W8_BF16 : W8_F16) : W8_F32;
     const int64_t t = blockIdx.x;
     for (int64_t h = (int64_t)threadIdx.x * 4; h < H; h += 1024) {
         const int left = (int)(H - h < 4 ? H - h : 4);
@@ -392,26 +391,21 @@ __global__ __launch_bounds__(256) void w8_combine_kernel(const void* __restrict_
         for (int j = 0; j < topk; ++j) {
             const int64_t p = t * topk + j;
             if ((uint32_t)ids[p] >= (uint32_t)E) continue;
-            const char* const o = reinterpret_cast<const char*>(O) + (p * H + h) * (OUT16 ? 2 : 4);
-            W8Raw<IN> r = {};
+            const float* const o = O + p * H + h;
+            float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             if (left == 4) {
-                __builtin_memcpy(&r, o, OUT16 ? 8 : 16);
+                __builtin_memcpy(r, o, 16);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (i < left) {
-                        if constexpr (OUT16) r.w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(o)[i] << (16 * (i & 1));
-                        else r.w[i] = reinterpret_cast<const uint32_t*>(o)[i];
-                    }
+                    if (i < left) r[i] = o[i];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += raw_value<IN>(r, i);
+            for (int i = 0; i < 4; ++i) v[i] += r[i];
         }
         store4<BF>(Y + t * H + h, v, left, (H & 3) == 0);
     }
 }
-
-constexpr int64_t kPairsFp32 = 64 << 20;        // bytes
 
 // Order of the grouped products' tiles.  A third to a half of the slots are empty, and with most experts at one tile every second one is: with the
 // rows fastest the workgroups that do work then land on every second place that the dispatcher deals out, which it does in turn,
@@ -425,7 +419,6 @@ struct W8MoeLayout {
     bool few;
     W8Kernel kernel;
     int bm, max_tiles;
-    bool out16;                 // the pairs' outputs in the activations' type
     size_t off_status, off_tops, off_h, off_xq, off_xs, off_sorted, off_token, off_tiles, off_hq, off_hs, off_o, total;
 };
 static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8MoeLayout* L) {
@@ -457,16 +450,13 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         L->off_hs = take((size_t)P * 4);
     } else {
         L->bm = w8_kernel_rows(L->kernel);
-        // A pair's weighted output is kept in fp32 while all of them fit the caches; beyond, in the activations' type (half of a step of it
-        // per pair, as the output itself): 4096 tokens to 8 experts each, 2048 features, 268 MB of fp32: 611 us for the layer against 702.
-        L->out16 = L->kernel == W8_TILE_128x256 && P * H * 4 > kPairsFp32;
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
         L->off_sorted = take((size_t)P * 4);
         L->off_token = take((size_t)P * 4);
         L->off_tiles = take((size_t)L->max_tiles * sizeof(TileDesc));
         L->off_hq = take((size_t)(P * fb));
         L->off_hs = take((size_t)P * 4);
-        L->off_o = take((size_t)P * H * (L->out16 ? 2 : 4));
+        L->off_o = take((size_t)P * H * 4);
     }
     L->total = off;
     return true;
@@ -560,8 +550,6 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.span = kSpan;
     t.x_rows = g.sorted_token;
     t.out = ws + L.off_h;
-    t.act_bf16 = bf;
-    t.out16 = L.out16;
     st = launch_w8_product(t, 1, L.kernel, s);
     if (st != MILO_OK) return st;
     q.in = ws + L.off_h;
@@ -581,8 +569,8 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     t.out = ws + L.off_o;
     st = launch_w8_product(t, 2, L.kernel, s);
     if (st != MILO_OK) return st;
-    auto combine = [&](auto kernel) { kernel<<<dim3((unsigned)T), dim3(256), 0, s>>>(ws + L.off_o, topk_ids, topk, E, H, Y); };
-    if (bf) combine(L.out16 ? w8_combine_kernel<true, true> : w8_combine_kernel<true, false>);
-    else combine(L.out16 ? w8_combine_kernel<false, true> : w8_combine_kernel<false, false>);
+    auto combine = [&](auto kernel) { kernel<<<dim3((unsigned)T), dim3(256), 0, s>>>(reinterpret_cast<const float*>(ws + L.off_o), topk_ids, topk, E, H, Y); };
+    if (bf) combine(w8_combine_kernel<true>);
+    else combine(w8_combine_kernel<false>);
     return launch_status();
 }

@@ -1,0 +1,52 @@
+"""The 8-bit path where its kernels could part from what is promised of them, against the 64-bit oracle (tolerances: see
+test_gpu_w8.py; what a test adds to them is derived beside it)."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from test_gpu_w8 import DTYPES, U, V, check_layer, check_linear, f64, make_layer, normal, routing, unblock
+from test_gpu_w8_kernels import kernel_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2504_02658_amd import api
+    return api
+
+
+# ---- the sum over a token's pairs --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H", [1024, 1001])
+def test_layer_of_many_pairs_adds_fp32_terms(api, H, dtype):
+    # 16800 pairs, 68 MB of them: as exact as a layer of a few tokens
+    T, F, E, topk = 2100, 64, 10, 8
+    layer, host = make_layer(api, H, F, E, seed=15)
+    X = normal(T, (T, H), dtype)
+    ids, gates = routing(T, E, topk, seed=13)
+    check_layer(layer.forward(X.cuda(), ids.cuda(), gates.cuda()), X, host, ids, gates)
+
+
+@pytest.mark.parametrize("T", [1, 16, 40, 2100])
+def test_layer_of_terms_beyond_fp16_that_cancel(api, T):
+    # Expert 2i + 1 has the down projection of expert 2i with the other sign, and a gate that is a 64th smaller.  Terms of
+    # up to some 10^6 leave a sum that fp16 holds.
+    H, F, E, topk = 1024, 64, 8, 8
+    host, dev = [], []
+    for e in range(0, E, 2):
+        W = [normal(e * 3 + i, s, torch.float32, std) for i, (s, std) in enumerate((((F, H), 0.05), ((F, H), 0.05), ((H, F), 6e3)))]
+        for sign in (1.0, -1.0):
+            ws = [W[0], W[1], W[2] * sign]
+            host.append([oracle.quantize_rows(w.numpy()) for w in ws])
+            dev.append(tuple(api.pack_w8(w.cuda()) for w in ws))
+    X = normal(7, (T, H), torch.float16)
+    ids = torch.stack([torch.randperm(E, generator=torch.Generator().manual_seed(t)) for t in range(T)]).to(torch.int32)
+    gates = torch.where(ids % 2 == 0, 1.0, 1.0 - 2.0 ** -6).float()
+    Y = api.W8MoELayer(dev, H, F).forward(X.cuda(), ids.cuda(), gates.cuda())
+    ref, _, terms = oracle.w8a8_moe(X.float().numpy(), host, ids.numpy(), gates.numpy())
+    assert terms.max() > 8 * 65504.0 and np.abs(ref).max() < 65504.0
+    assert torch.isfinite(Y).all()
+    check_layer(Y, X, host, ids, gates)
