@@ -450,8 +450,8 @@ int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H,
  *   workspace    milo_moe_w8a8_workspace(T, H, F, E, topk) bytes (0 if the shape is invalid), scratch
  * An id outside 0..E-1 contributes nothing; an expert without
  * tokens is legal, and a token without any gets zeros.  Two runs give bit-identical results.
- * Limits: as the linear's for [F x H] and [H x F]; T < 2^23, E max(H, F) <= 2^27; the codes of T rows of H and of T topk rows of
- * F within 4 GiB each.  A routed pair's weighted output stays fp32 until it is added to its token's sum, whose rounding to the output type is the only one.
+ * Limits: as the linear's for [F x H] and [H x F]; T < 2^23, E max(H, F) <= 2^27, (T topk / 128 + 1 + E) (max(F / 128, H / 256) + 1) <= 2^22 (more
+ * may pass; milo_moe_w8a8_workspace says so); the codes of T rows of H and of T topk rows of F within 4 GiB each.  A routed pair's weighted output stays fp32 until it is added to its token's sum, whose rounding to the output type is the only one.
  * Errors: NULL, SHAPE (also unknown flags), WORKSPACE, ALIGN, HIP.
  */
 size_t milo_moe_w8a8_workspace(int64_t T, int64_t H, int64_t F, int E, int topk);

@@ -377,7 +377,8 @@ static int launch_tile(W8TileArgs a, hipStream_t stream) {
     }
     if (EPI == 0) a.m_tiles = (int)((a.M + BM - 1) / BM);
     a.n_tiles = (int)((a.N + OUTN - 1) / OUTN);
-    if ((int64_t)a.m_tiles * a.n_tiles > (int64_t(1) << 31) / (WM * WN * WK * 64)) return MILO_ERR_SHAPE;
+    static_assert(WM * WN * WK <= 8, "512 threads");
+    if ((int64_t)a.m_tiles * a.n_tiles > kW8MaxGroups) return MILO_ERR_SHAPE;
     w8_tile_kernel<WM, WN, WK, TM, TN, NS, EPI, BF><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(WM * WN * WK * 64), lds, stream>>>(a);
     return launch_status();
 }
@@ -404,6 +405,15 @@ int w8_kernel_rows(W8Kernel k) {
         case W8_WIDE_16x16: case W8_WIDE_16x32: case W8_WIDE_16x64: return 16;
         case W8_WIDE_32x32: case W8_WIDE_32x64: return 32;
         case W8_WIDE_64x64: case W8_TILE_64x128: return 64;
+        default: return 128;
+    }
+}
+int w8_kernel_cols(W8Kernel k) {
+    switch (k) {
+        case W8_WIDE_16x16: return 16;
+        case W8_WIDE_16x32: case W8_WIDE_32x32: return 32;
+        case W8_WIDE_16x64: case W8_WIDE_32x64: case W8_WIDE_64x64: return 64;
+        case W8_TILE_128x256: return 256;
         default: return 128;
     }
 }

@@ -425,7 +425,7 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     if (T < 1 || E < 1 || E > 65536 || topk < 1 || topk > E) return false;
     if (!w8_shape_ok(F, H) || !w8_shape_ok(H, F)) return false;
     if (T >= (int64_t(1) << 23) || T > (int64_t(1) << 30) / topk) return false;
-    if (E > (int64_t(1) << 27) / (H > F ? H : F)) return false;         // (the grid's work items fit 32 bits)
+    if (E > (int64_t(1) << 27) / (H > F ? H : F)) return false;
     const int64_t P = T * topk, hb = w8_kblocks(H) * 64, fb = w8_kblocks(F) * 64;
     // rows of codes are addressed with 32-bit offsets
     if (T * hb >= 0xFFFF0000ll || P * fb >= 0xFFFF0000ll) return false;
@@ -441,6 +441,14 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     // 128 x 256, us: 8 experts of 14336 x 4096, 10 rows each 260 and 293, 16 rows 268 and 296, 24 rows 288 and 305; 66 of 1408 x 2048, 8 rows 135 and
     // 143, 19 rows 151 and 153, 31 rows 169 and 161.
     L->kernel = P < 24 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
+    // The grid has workgroups for every slot of the list of tiles, some of them empty.  Where those of the small tiles are too many (thousands of
+    // experts of long rows), the large ones, which are a quarter as many, serve; where those are, the call is refused before it launches anything.
+    auto fits = [&](W8Kernel k) {       // gate and up (half as many features of either), down
+        const int64_t slots = (P + w8_kernel_rows(k) - 1) / w8_kernel_rows(k) + E, up = w8_kernel_cols(k) / 2, down = w8_kernel_cols(k);
+        return slots * ((F + up - 1) / up) <= kW8MaxGroups && slots * ((H + down - 1) / down) <= kW8MaxGroups;
+    };
+    if (!L->few && !fits(L->kernel)) L->kernel = W8_TILE_128x256;
+    if (!L->few && !fits(L->kernel)) return false;
     L->off_h = take((size_t)P * F * 4);
     L->off_xq = take((size_t)(T * hb));
     L->off_xs = take((size_t)T * 4);
@@ -573,4 +581,11 @@ extern "C" int milo_moe_w8a8_forward(const milo_half* X, int64_t T, int64_t H, i
     if (bf) combine(w8_combine_kernel<true>);
     else combine(w8_combine_kernel<false>);
     return launch_status();
+}
+
+// For the tests: the kernel of a layer's grouped products (W8Kernel), -1 for those of a few tokens, -2 for a shape that is refused.
+extern "C" int milo_moe_w8a8_route(int64_t T, int64_t H, int64_t F, int E, int topk) {
+    W8MoeLayout L;
+    if (!w8_moe_layout(T, H, F, E, topk, &L)) return -2;
+    return L.few ? -1 : (int)L.kernel;
 }

@@ -202,7 +202,8 @@ static int launch_wide(W8TileArgs a, hipStream_t stream) {
     }
     if (EPI == 0) a.m_tiles = (int)((a.M + TM * 16 - 1) / (TM * 16));
     a.n_tiles = (int)((a.N + OUTN - 1) / OUTN);
-    if ((int64_t)a.m_tiles * a.n_tiles > (int64_t(1) << 31) / (kWideWaves * 64)) return MILO_ERR_SHAPE;
+    static_assert(kWideWaves == 8, "512 threads");
+    if ((int64_t)a.m_tiles * a.n_tiles > kW8MaxGroups) return MILO_ERR_SHAPE;
     w8_wide_kernel<TM, RN, EPI, BF, STAGED><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(kWideWaves * 64), lds, stream>>>(a);
     return launch_status();
 }

@@ -50,3 +50,19 @@ def test_layer_of_terms_beyond_fp16_that_cancel(api, T):
     assert terms.max() > 8 * 65504.0 and np.abs(ref).max() < 65504.0
     assert torch.isfinite(Y).all()
     check_layer(Y, X, host, ids, gates)
+
+
+# ---- many experts ------------------------------------------------------------------------------------------------
+
+def test_layer_of_more_experts_than_small_tiles_have_a_grid_for(api):
+    # 8192 experts with 16384 features: 2^22 workgroups of 32 features and one slot's more.  (The experts share three sets of weights.)
+    T, H, F, E = 17, 64, 16384, 8192
+    some, hosts = make_layer(api, H, F, 3, seed=40)
+    layer = api.W8MoELayer([some.experts[e % 3] for e in range(E)], H, F)
+    X = normal(3, (T, H), torch.float16)
+    ids = ((torch.arange(T) * 997 + 8191) % E).to(torch.int32).view(T, 1)
+    gates = torch.rand((T, 1), generator=torch.Generator().manual_seed(1)) + 0.1
+    assert len(set(ids.flatten().tolist())) == T and int(ids.max()) == E - 1
+    Y = layer.forward(X.cuda(), ids.cuda(), gates.cuda())
+    assert layer.routing_status() == 0
+    check_layer(Y, X, hosts, ids % 3, gates)
