@@ -29,7 +29,7 @@ __host__ __device__ inline int64_t w8_code_bytes(int64_t R, int64_t K) { return 
 // ---------------------------------------------------------------------------------------------
 // Quantizing a row: s = fp32(top / 127), code = round-half-even(x / s) of the exact quotient.
 struct RowStep {
-    float s, inv, half;     // scale; 1 / s, or 0 for a row whose codes are all zero; s / 2
+    float s, inv, lim;      // scale; 1 / s, or 0 for a row whose codes are all zero; what twice a remainder is compared with: s, or infinity for such a row
 };
 // `top_bits`: largest magnitude of the row as the bits of an fp32 number (an infinity or a NaN, whose bits are the
 // largest, marks the row).  A row with such a value gets the scale NaN, so that everything computed from it is NaN;
@@ -38,24 +38,25 @@ __device__ __forceinline__ RowStep row_step(uint32_t top_bits) {
     RowStep r;
     r.s = __uint_as_float(top_bits) / 127.0f;
     r.inv = 0.0f;
-    r.half = __uint_as_float(0x7f800000u);
+    r.lim = __uint_as_float(0x7f800000u);
     if (top_bits >= 0x7f800000u) {
         r.s = __uint_as_float(0x7fc00000u);
     } else if (r.s < 0x1p-126f) {
         r.s = 0.0f;
     } else {
         r.inv = 1.0f / r.s;
-        r.half = 0.5f * r.s;
+        r.lim = r.s;
     }
     return r;
 }
 // The product with 1/s is off by at most two units in the last place of a number below 2^7, so its rounding is the code or a neighbour
-// of it.  x - c s is a multiple of half a unit in the last place of s and at most about s/2, hence exact in fp32, and
-// comparing it with s/2 settles the code, ties included, without a division.
+// of it.  x - c s is a multiple of half a unit in the last place of s (of a whole one in the lowest binade) and at most about s/2, hence exact
+// in fp32, and comparing its double with s settles the code, ties included, without a division.  (s/2 need not be a number: 2^-126 is the
+// smallest scale, and half of an odd one below 2^-125 has no fp32.)
 __device__ __forceinline__ int row_code(float x, const RowStep& r) {
-    const float c = rintf(x * r.inv), d = fmaf(-c, r.s, x), far = fabsf(d);
+    const float c = rintf(x * r.inv), d = fmaf(-c, r.s, x), far = 2.0f * fabsf(d);
     const int q = (int)c, away = d > 0.0f ? 1 : -1;
-    const bool other = (far > r.half) | ((far == r.half) & ((q & 1) != 0));
+    const bool other = (far > r.lim) | ((far == r.lim) & ((q & 1) != 0));
     return r.inv > 0.0f ? q + (other ? away : 0) : 0;
 }
 __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
@@ -81,7 +82,7 @@ __device__ __forceinline__ u32x4 row_codes16(const float (&v)[16], const RowStep
     u32x4 o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = low_bytes(b[4 * i], b[4 * i + 1], b[4 * i + 2], b[4 * i + 3]);
-    if (far >= r.half) {
+    if (2.0f * far >= r.lim) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             o[i] = pack4(row_code(v[4 * i], r), row_code(v[4 * i + 1], r), row_code(v[4 * i + 2], r), row_code(v[4 * i + 3], r));

@@ -66,3 +66,21 @@ def test_layer_of_more_experts_than_small_tiles_have_a_grid_for(api):
     Y = layer.forward(X.cuda(), ids.cuda(), gates.cuda())
     assert layer.routing_status() == 0
     check_layer(Y, X, hosts, ids % 3, gates)
+
+
+# ---- the quantizer -----------------------------------------------------------------------------------------------
+
+def test_pack_next_to_ties_at_the_smallest_scales(api):
+    # scales of odd 24-bit numbers S in [2^-126, 2^-125): half of one is no fp32 number.  Units of 2^-149; values next to (n + 1/2) S.
+    rng = np.random.default_rng(3)
+    S = rng.integers(1 << 22, 1 << 23, 62) * 2 + 1
+    S = np.concatenate([[15502097, (1 << 24) - 1], S]).astype(np.int64)
+    rows = []
+    for s in S:
+        near = [(2 * n + 1) * s // 2 + d for n in range(0, 126) for d in (0, 1)]
+        rows.append([127 * s] + near + [-v for v in near])
+    W = (np.array(rows).astype(np.float64) * 2.0 ** -149).astype(np.float32)
+    oc, os_ = oracle.quantize_rows(W)
+    assert (os_ >= np.float32(2.0 ** -126)).all() and (os_ < np.float32(2.0 ** -125)).all()
+    c, s = unblock(api.pack_w8(torch.from_numpy(W).cuda()).w8, *W.shape)
+    assert np.array_equal(s, os_) and np.array_equal(c, oc)
