@@ -89,17 +89,18 @@ __device__ __forceinline__ u32x4 row_codes16(const float (&v)[16], const RowStep
     }
     return o;
 }
-// The same for values that carry a rounding of their own (the SwiGLU output): the product's rounding is as good as any.
-__device__ __forceinline__ u32x4 near_codes16(const float (&v)[16], float inv) {
-    u32x4 o;
+// Four codes, by the same rule.
+__device__ __forceinline__ uint32_t row_codes4(const float (&v)[4], const RowStep& r) {
+    uint32_t b[4];
+    float far = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t b[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(fmaf(v[4 * i + j], inv, kRoundMagic));
-        o[i] = low_bytes(b[0], b[1], b[2], b[3]);
+        const float t = fmaf(v[i], r.inv, kRoundMagic);
+        b[i] = __float_as_uint(t);
+        far = fmaxf(far, fabsf(fmaf(-(t - kRoundMagic), r.s, v[i])));
     }
-    return o;
+    if (2.0f * far >= r.lim) return pack4(row_code(v[0], r), row_code(v[1], r), row_code(v[2], r), row_code(v[3], r));
+    return low_bytes(b[0], b[1], b[2], b[3]);
 }
 
 // Element types of what is quantized.

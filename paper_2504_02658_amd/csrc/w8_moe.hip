@@ -292,11 +292,7 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = k + j < a.F ? h[j] : 0.0f;
             }
-            uint32_t b[4];
-            const float inv = s_step[p].inv;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(fmaf(v[j], inv, kRoundMagic));
-            *reinterpret_cast<uint32_t*>(codes + i * 4) = low_bytes(b[0], b[1], b[2], b[3]);
+            *reinterpret_cast<uint32_t*>(codes + i * 4) = row_codes4(v, s_step[p]);
         }
         __syncthreads();
     }

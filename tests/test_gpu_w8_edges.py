@@ -84,3 +84,31 @@ def test_pack_next_to_ties_at_the_smallest_scales(api):
     assert (os_ >= np.float32(2.0 ** -126)).all() and (os_ < np.float32(2.0 ** -125)).all()
     c, s = unblock(api.pack_w8(torch.from_numpy(W).cuda()).w8, *W.shape)
     assert np.array_equal(s, os_) and np.array_equal(c, oc)
+
+
+# ---- SwiGLU rows -------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T", [8, 16, 40, 700])
+def test_layer_codes_of_swiglu_rows_at_ties(api, T):
+    # x = (1, 0, 127, 0 ..), gate weights (32, 0, 0, 127 * 32), up weights (t, 0, 0, 127 t): codes (1, 0, 0, 127), so gate = 32,
+    # SiLU(32) = 32 in fp32, up = t, and the SwiGLU row is 32 t, exactly.  It is 127 s and all (n + 1/2) s, with s no power of two.
+    # The down projection copies it out: its codes show, and have to be those of the exact quotients, ties to even.
+    H = F = 128
+    S = [3, 5, 7, 11, 101, 333, 1021, 511]
+    want, dev = [], []
+    for s in S:
+        h = np.concatenate([[127.0], np.arange(-63, 64) + 0.5]) * (s * 2.0 ** -9)
+        t = torch.from_numpy(h / 32).float()
+        W1, W3 = torch.zeros((F, H)), torch.zeros((F, H))
+        W1[:, 0], W1[:, 3] = 32.0, 127.0 * 32.0
+        W3[:, 0], W3[:, 3] = t, 127.0 * t
+        assert np.array_equal(W3[:, 3].double().numpy(), 127.0 * h / 32)
+        want.append(oracle.quantize_rows(h[None].astype(np.float32))[0][0])
+        dev.append(tuple(api.pack_w8(w.cuda()) for w in (W1, W3, torch.eye(H))))
+    X = torch.zeros((T, H), dtype=torch.bfloat16)
+    X[:, 0], X[:, 2] = 1.0, 127.0
+    ids = (torch.arange(T) % len(S)).to(torch.int32).view(T, 1)
+    Y = f64(api.W8MoELayer(dev, H, F).forward(X.cuda(), ids.cuda(), torch.ones((T, 1)).cuda()))
+    for t in range(T):
+        got = Y[t] / (S[t % len(S)] * 2.0 ** -9)            # (the output's rounding: at most 127 * 2^-8 < 1/2)
+        assert np.array_equal(np.rint(got), want[t % len(S)]), (t, S[t % len(S)])
