@@ -177,7 +177,6 @@ __global__ __launch_bounds__(kGateThreads) void moe_gate_token_kernel(const Gate
 // blocks of 32, of which lane (row, q) holds elements 8q .. 8q + 7 of its row, so that step j multiplies element j of every quarter.
 // The rate of those instructions bounds it (64 multiplications per cycle and compute unit).
 constexpr int kGateTileWaves = 8, kGateTileExperts = 256;
-typedef double f64x4 __attribute__((ext_vector_type(4)));
 template <int IN, int TILES>
 __global__ __launch_bounds__(kGateTileWaves * 64) void moe_gate_tile_kernel(const GateArgs a) {
     __shared__ double s_logit[16][kGateTileExperts];

@@ -14,6 +14,7 @@ namespace milo {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* LdsDst;
 // A pointer that was read from memory (an expert table's) says nothing about its address space, and a load through it would count as an
 // LDS operation too: fragments go through these.

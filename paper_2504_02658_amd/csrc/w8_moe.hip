@@ -212,8 +212,8 @@ __global__ __launch_bounds__(kFewUpThreads, 4) void w8_few_up_kernel(const W8Few
     if (mine && c16 == 0) a.tops[row * ((a.F + 15) / 16) + blockIdx.x] = top;
 }
 
-// The runs of all experts' weights are one sequence, which the waves share; the products of a run are added up in integers and
-// turned to fp32 at its end.
+// The runs of all experts' weights are one sequence, which the waves share.  The products of a run are added up in integers; what one expert's runs
+// add up to, and the experts, in 64 bits: a linear's sum is to be that of the integers, and its pieces may cancel.
 template <bool BF, bool STAGED>
 __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W8FewArgs a) {
     constexpr int NW = kFewDownThreads / 64, B = kFewDownRun;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
     __shared__ __attribute__((aligned(16))) float s_sw[kFewMaxPairs][16];   // the scales of this workgroup's features,
     __shared__ int32_t s_row[kFewMaxPairs][kFewTokens];             // its tokens' rows (-1: none)
     __shared__ float s_factor[kFewMaxPairs][kFewTokens];            // and the rows' scales times the gates
-    __shared__ f32x4 s_part[NW][64];
+    __shared__ f64x4 s_part[NW][64];
     extern __shared__ __attribute__((aligned(16))) unsigned char codes[];   // piece c of 16 columns of pair p: at (c * P + p) * 16
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kb = (int)w8_kblocks(a.F), P = a.T * a.topk;
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
         }
         __syncthreads();
     }
-    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    f64x4 y = {0.0, 0.0, 0.0, 0.0};
     auto work = [&](int r, int from) {
         const int s = r / runs, u = (r - s * runs) * B;
         const float f = s_factor[s][m];
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
 #pragma unroll
         for (int i = 0; i < B; ++i) acc = mfma16_i8(w[from][i], q[from][i], acc);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += row >= 0 ? (float)acc[i] * f * sw[i] : 0.0f;      // (another token's expert may have a scale that is no number)
+        for (int i = 0; i < 4; ++i) y[i] += row >= 0 ? (double)acc[i] * ((double)f * (double)sw[i]) : 0.0;      // (another token's expert may have a scale that is no number)
     };
     for (int r = wave; r < all; r += 2 * NW) {
         work(r, 0);
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(kFewDownThreads, 4) void w8_few_down_kernel(const W
     if (wave != 0 || m >= a.T || n >= a.H) return;
 #pragma unroll
     for (int i = 1; i < NW; ++i) y += s_part[i][lane];
-    const float v[4] = {y[0], y[1], y[2], y[3]};
+    const float v[4] = {(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
     store4<BF>(a.Y + m * a.H + n, v, (int)(a.H - n < 4 ? a.H - n : 4), (a.H & 3) == 0);
 }
 template <bool BF, bool STAGED>

@@ -112,3 +112,18 @@ def test_layer_codes_of_swiglu_rows_at_ties(api, T):
     for t in range(T):
         got = Y[t] / (S[t % len(S)] * 2.0 ** -9)            # (the output's rounding: at most 127 * 2^-8 < 1/2)
         assert np.array_equal(np.rint(got), want[t % len(S)]), (t, S[t % len(S)])
+
+
+@pytest.mark.parametrize("T", [2, 20, 300])
+def test_layer_down_sums_that_cancel(api, T):
+    # The second half of the features is the first half with the down projection's sign turned: every integer sum is zero, whatever
+    # pieces of it the waves add up.  (Pieces added in 64 bits leave less than 2^-48 of their magnitude.)
+    H, D = 64, 2560
+    W1, W3, W2 = normal(1, (D, H), std=0.2), normal(2, (D, H), std=0.2), normal(3, (H, D), std=0.2)
+    pack = lambda *ws: tuple(api.pack_w8(w.cuda()) for w in ws)
+    two, one = pack(torch.cat([W1, W1]), torch.cat([W3, W3]), torch.cat([W2, -W2], 1)), pack(torch.cat([W1, W1]), torch.cat([W3, W3]), torch.cat([W2, 0 * W2], 1))
+    X = normal(T, (T, H), torch.bfloat16).cuda()
+    ids, gates = torch.zeros((T, 1), dtype=torch.int32, device="cuda"), torch.rand((T, 1), device="cuda") + 0.5
+    half = f64(api.W8MoELayer([one], H, 2 * D).forward(X, ids, gates))
+    Y = f64(api.W8MoELayer([two], H, 2 * D).forward(X, ids, gates))
+    assert np.abs(half).max() > 1.0 and np.abs(Y).max() <= 2.0 ** -40 * np.abs(half).max()
