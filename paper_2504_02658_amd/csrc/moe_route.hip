@@ -95,11 +95,12 @@ __device__ __forceinline__ void choose_experts(const double* logits, int64_t t, 
     // (a NaN logit, infinite ones or a NaN in the inputs: every gate of the token is NaN, as the quotient gives)
     double sum = 0.0;
     bool nan = false;
-    const double mine = lane < a.topk ? (double)expf((float)(my_logit - top)) : 0.0;
+    // exp in 64 bits: rounded to fp32, the argument of an expert far from the top would move its gate by the distance's own rounding.
+    const double mine = lane < a.topk ? exp(my_logit - top) : 0.0;
     for (int e = lane; e < a.E; e += 64) {
         const double l = logits[e];
         nan = nan || l != l;
-        if (!a.renormalize) sum += (double)expf((float)(l - top));
+        if (!a.renormalize) sum += exp(l - top);
     }
     if (a.renormalize) sum = mine;
     if (nan) sum = __builtin_nan("");

@@ -127,3 +127,18 @@ def test_layer_down_sums_that_cancel(api, T):
     half = f64(api.W8MoELayer([one], H, 2 * D).forward(X, ids, gates))
     Y = f64(api.W8MoELayer([two], H, 2 * D).forward(X, ids, gates))
     assert np.abs(half).max() > 1.0 and np.abs(Y).max() <= 2.0 ** -40 * np.abs(half).max()
+
+
+# ---- router ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("T,H,E,topk", [(3, 200, 40, 40), (33, 2048, 64, 6), (1100, 200, 40, 40), (1100, 2048, 64, 6), (1030, 64, 257, 64)])
+def test_route_gates_are_rounded_once(api, T, H, E, topk, renormalize, dtype):
+    # logits some tens to a hundred apart; exp, its sums and the quotient carry a few units of 2^-53, the logits' sums H of them
+    # relative to their terms: below 2^-34 of a gate, so what counts is the rounding to fp32
+    X, Wg = normal(T + H, (T, H), dtype), normal(E + H, (E, H), dtype, 20.0 / H ** 0.5)
+    ids, gates = api.moe_route(X.cuda(), Wg.cuda(), topk, renormalize=renormalize)
+    oi, og = oracle.moe_route(X.float().numpy(), Wg.float().numpy(), topk, renormalize, 0)
+    assert np.array_equal(ids.cpu().numpy(), oi)
+    assert (np.abs(gates.cpu().double().numpy() - og) <= og * V * (1 + 2.0 ** -9) + 2.0 ** -150).all()
