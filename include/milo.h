@@ -418,9 +418,10 @@ int milo_w8a8_gemm(const milo_half* X, int64_t M, int64_t N, int64_t K, const vo
  *   ids   out, [T x (topk + n_shared)] int32;  gates  out, the same shape, fp32
  * The softmax runs over all E experts, with MILO_ROUTE_RENORMALIZE over the chosen ones (their weights then add up to one).
  * n_shared always-on experts are appended as columns with ids E, E+1, .. and gate 1: the columns milo_moe_w3lr_forward and
- * milo_moe_w8a8_forward take.  The logits are formed and compared in 64 bits, so the choice does not depend on the order of
- * the summation.  A NaN logit ranks below every other one (the ids stay distinct and in range) and makes all gates of its token NaN;
- * so does an infinite largest logit.
+ * milo_moe_w8a8_forward take.  The logits are 64-bit sums of exact products.  While every partial sum fits 53 bits they are exact, and
+ * equal ones are equal whatever order they were added in; beyond (bfloat16 rows whose products lie many binades apart) two that differ by
+ * 64-bit rounding may be taken in either order, which may change with T.  A NaN logit ranks below every other one (the ids stay distinct
+ * and in range) and makes all gates of its token NaN; so does an infinite largest logit.
  * Limits: E <= 1024, topk <= min(E, 64), n_shared <= 64, T < 2^22, H <= 2^20.
  * Errors: NULL, SHAPE (also unknown flags), ALIGN, HIP.
  */

@@ -4,7 +4,8 @@
 //   gates = exp(l_chosen - max l) / sum over all experts (or over the chosen ones) of exp(l - max l)
 //
 // Whether two logits are in one order or the other decides which weights a token meets, so the sums are held in 64 bits:
-// products of two 16-bit numbers are exact there, and the choice does not hang on the order of the summation.
+// products of two 16-bit numbers are exact there, and so are the sums while they fit 53 bits.  (The kernels below add in different orders: beyond
+// that, logits that differ by 64-bit rounding may change places between them.)
 #include "milo_host.h"
 #include "w8_kernels.h"
 

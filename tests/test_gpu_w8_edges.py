@@ -142,3 +142,19 @@ def test_route_gates_are_rounded_once(api, T, H, E, topk, renormalize, dtype):
     oi, og = oracle.moe_route(X.float().numpy(), Wg.float().numpy(), topk, renormalize, 0)
     assert np.array_equal(ids.cpu().numpy(), oi)
     assert (np.abs(gates.cpu().double().numpy() - og) <= og * V * (1 + 2.0 ** -9) + 2.0 ** -150).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [5, 1030])
+def test_route_of_equal_sums_of_different_terms(api, T, dtype):
+    # Experts in threes whose rows are each other's, permuted in pairs of columns that a token's activations do not tell apart: the sums are equal, their
+    # terms come in another order, and all of them fit 53 bits.  Equal ones: the lowest id.
+    H, E = 600, 30
+    g = torch.Generator().manual_seed(T)
+    X = torch.randint(-8, 9, (T, H // 2), generator=g).repeat(1, 2).to(dtype)
+    W = torch.randint(-8, 9, (E // 3, H), generator=g)
+    swap = torch.cat([W[:, H // 2:], W[:, :H // 2]], 1)
+    half = torch.where(torch.arange(H) % (H // 2) % 2 == 0, W, swap)
+    Wg = torch.stack([W, swap, half], 1).view(E, H).to(dtype)
+    ids, _ = api.moe_route(X.cuda(), Wg.cuda(), 12)
+    assert np.array_equal(ids.cpu().numpy(), oracle.moe_route(X.float().numpy(), Wg.float().numpy(), 12, True, 0)[0])
