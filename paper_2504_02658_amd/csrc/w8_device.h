@@ -110,22 +110,11 @@ template <int IN> struct W8Raw { uint32_t w[IN == W8_F32 ? 16 : 8]; };      // 1
 
 // Elements [k, k + 16) of a row of K, zeros beyond it.  The row may start at any element's address: whole pieces are
 // copied by the widest loads (which need no alignment here), the last one element by element.
-// WHOLE: the piece is known to lie inside, and the row to start at a 16-byte boundary.
-template <int IN, bool WHOLE = false>
+template <int IN>
 __device__ __forceinline__ W8Raw<IN> load16(const void* row, int64_t k, int64_t K) {
     constexpr int SZ = IN == W8_F32 ? 4 : 2;
     W8Raw<IN> r;
     const char* p = reinterpret_cast<const char*>(row) + k * SZ;
-    if constexpr (WHOLE) {
-        const u32x4* const q = reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-        for (int i = 0; i < SZ; ++i) {
-            const u32x4 v = q[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) r.w[4 * i + j] = v[j];
-        }
-        return r;
-    }
     if (k + 16 <= K) {
         __builtin_memcpy(&r, p, 16 * SZ);
     } else {

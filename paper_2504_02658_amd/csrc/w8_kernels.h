@@ -43,8 +43,6 @@ struct W8TileArgs {
 };
 // The kernels of a product, named by rows x features of a workgroup (EPI 1: half as many output features, from gate and up).
 enum W8Kernel { W8_WIDE_16x16, W8_WIDE_16x32, W8_WIDE_16x64, W8_WIDE_32x32, W8_WIDE_32x64, W8_WIDE_64x64, W8_TILE_64x128, W8_TILE_128x128, W8_TILE_128x256 };
-int w8_kernel_rows(W8Kernel k);
-int w8_kernel_cols(W8Kernel k);
 constexpr int64_t kW8MaxGroups = int64_t(1) << 22;      // workgroups of a product, of 512 threads at most: 2^31 work items
 int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream);
 // Up to 16 rows whose codes fit kW8WideStaged bytes, in one launch: a.A is the 16-bit activations, k one of the kernels of 16 rows.  (Every

@@ -400,23 +400,6 @@ static int launch_w8_tile(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t 
         return launch_tile<2, 4, 1, 2, 1, 4, 2, false>(a, stream);
     return launch_tile<2, 4, 1, 2, 2, 3, 2, false>(a, stream);
 }
-int w8_kernel_rows(W8Kernel k) {
-    switch (k) {
-        case W8_WIDE_16x16: case W8_WIDE_16x32: case W8_WIDE_16x64: return 16;
-        case W8_WIDE_32x32: case W8_WIDE_32x64: return 32;
-        case W8_WIDE_64x64: case W8_TILE_64x128: return 64;
-        default: return 128;
-    }
-}
-int w8_kernel_cols(W8Kernel k) {
-    switch (k) {
-        case W8_WIDE_16x16: return 16;
-        case W8_WIDE_16x32: case W8_WIDE_32x32: return 32;
-        case W8_WIDE_16x64: case W8_WIDE_32x64: case W8_WIDE_64x64: return 64;
-        case W8_TILE_128x256: return 256;
-        default: return 128;
-    }
-}
 int launch_w8_product(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t stream) {
     switch (k) {
         case W8_WIDE_16x16: return launch_w8_wide(a, epi, 1, 1, stream);

@@ -439,8 +439,9 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
     L->kernel = P < 24 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
     // The grid has workgroups for every slot of the list of tiles, some of them empty.  Where those of the small tiles are too many (thousands of
     // experts of long rows), the large ones, which are a quarter as many, serve; where those are, the call is refused before it launches anything.
+    auto tile_rows = [](W8Kernel k) { return k == W8_WIDE_32x64 ? 32 : 128; };
     auto fits = [&](W8Kernel k) {       // gate and up (half as many features of either), down
-        const int64_t slots = (P + w8_kernel_rows(k) - 1) / w8_kernel_rows(k) + E, up = w8_kernel_cols(k) / 2, down = w8_kernel_cols(k);
+        const int64_t slots = (P + tile_rows(k) - 1) / tile_rows(k) + E, down = k == W8_WIDE_32x64 ? 64 : 256, up = down / 2;
         return slots * ((F + up - 1) / up) <= kW8MaxGroups && slots * ((H + down - 1) / down) <= kW8MaxGroups;
     };
     if (!L->few && !fits(L->kernel)) L->kernel = W8_TILE_128x256;
@@ -453,7 +454,7 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         L->off_hq = take((size_t)(P * fb));
         L->off_hs = take((size_t)P * 4);
     } else {
-        L->bm = w8_kernel_rows(L->kernel);
+        L->bm = tile_rows(L->kernel);
         L->max_tiles = (int)((P + L->bm - 1) / L->bm) + E;
         L->off_sorted = take((size_t)P * 4);
         L->off_token = take((size_t)P * 4);

@@ -207,14 +207,12 @@ static int launch_wide(W8TileArgs a, hipStream_t stream) {
     w8_wide_kernel<TM, RN, EPI, BF, STAGED><<<dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(kWideWaves * 64), lds, stream>>>(a);
     return launch_status();
 }
-template <int EPI, bool BF>
-static int launch_wide_shape(const W8TileArgs& a, int tm, int rn, hipStream_t stream) {
-    if constexpr (EPI == 0) {
-        if (tm == 4) return launch_wide<4, 4, EPI, BF>(a, stream);
-    }
-    if (tm == 2) return rn == 4 ? launch_wide<2, 4, EPI, BF>(a, stream) : launch_wide<2, 2, EPI, BF>(a, stream);
-    if (rn == 4) return launch_wide<1, 4, EPI, BF>(a, stream);
-    return rn == 2 || EPI == 1 ? launch_wide<1, 2, EPI, BF>(a, stream) : launch_wide<1, EPI == 1 ? 2 : 1, EPI, BF>(a, stream);
+template <bool BF>
+static int launch_wide_linear(const W8TileArgs& a, int tm, int rn, hipStream_t stream) {
+    if (tm == 4) return launch_wide<4, 4, 0, BF>(a, stream);
+    if (tm == 2) return rn == 4 ? launch_wide<2, 4, 0, BF>(a, stream) : launch_wide<2, 2, 0, BF>(a, stream);
+    if (rn == 4) return launch_wide<1, 4, 0, BF>(a, stream);
+    return rn == 2 ? launch_wide<1, 2, 0, BF>(a, stream) : launch_wide<1, 1, 0, BF>(a, stream);
 }
 template <bool BF>
 static int launch_staged(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
@@ -226,8 +224,9 @@ int launch_w8_staged(const W8TileArgs& a, W8Kernel k, hipStream_t stream) {
     return a.act_bf16 ? launch_staged<true>(a, k, stream) : launch_staged<false>(a, k, stream);
 }
 int launch_w8_wide(const W8TileArgs& a, int epi, int tm, int rn, hipStream_t stream) {
-    if (epi == 0) return a.act_bf16 ? launch_wide_shape<0, true>(a, tm, rn, stream) : launch_wide_shape<0, false>(a, tm, rn, stream);
-    return epi == 1 ? launch_wide_shape<1, false>(a, tm, rn, stream) : launch_wide_shape<2, false>(a, tm, rn, stream);
+    if (epi == 0) return a.act_bf16 ? launch_wide_linear<true>(a, tm, rn, stream) : launch_wide_linear<false>(a, tm, rn, stream);
+    if (tm != 2 || rn != 4) return MILO_ERR_SHAPE;          // (experts: this shape alone)
+    return epi == 1 ? launch_wide<2, 4, 1, false>(a, stream) : launch_wide<2, 4, 2, false>(a, stream);
 }
 
 }  // namespace milo
