@@ -378,8 +378,8 @@ int milo_moe_w3lr_routing_status(const void* workspace, void* stream);
  *     scale = fp32(max |v| / 127) over the row,   code = round-half-even(v / scale)  of the exact quotient
  * and the linear is
  *     Y[m,n] = (sum over k of code_x[m,k] code_w[n,k]) * scale_x[m] * scale_w[n]
- * with the sum exact in 32-bit integers (whatever the order), its products with the scales in fp32 and one rounding to
- * the output type.  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale
+ * with the sum exact in 32-bit integers (whatever the order), its products with the scales in fp32, scale_x first, and one
+ * rounding to the output type (bfloat16 activations: within fp32's range while K times their largest magnitude is below 2^120).  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale
  * NaN, so that what is computed from it is NaN and nothing else is touched.
  * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M < 2^22, N K, M K and M N <= 2^36; nothing has to
  * be a multiple of anything.  Pointers are 16-byte aligned, arrays dense.  These calls need no prepared workspace: theirs is scratch

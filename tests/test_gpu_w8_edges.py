@@ -129,6 +129,66 @@ def test_layer_down_sums_that_cancel(api, T):
     assert np.abs(half).max() > 1.0 and np.abs(Y).max() <= 2.0 ** -40 * np.abs(half).max()
 
 
+# ---- long rows and large values ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N,K,dtype", [(3, 65537, torch.float32), (17, 65600, torch.float16), (2, 131071, torch.bfloat16), (5, 131072, torch.float32),
+                                       (1030, 65600, torch.float16), (1024, 66000, torch.bfloat16)])
+def test_pack_of_rows_longer_than_the_registers_hold(api, N, K, dtype):
+    # beyond 65536 columns a row is read twice; every code of varied rows, few rows and many
+    W = normal(N + K, (N, K), dtype, 0.05)
+    W[0, K - 1], W[N - 1, 65536] = 2.0, -3.0
+    c, s = unblock(api.pack_w8(W.cuda()).w8, N, K)
+    oc, os_ = oracle.quantize_rows(W.float().numpy())
+    assert np.array_equal(c, oc) and np.array_equal(s, os_)
+
+
+LONG = [("wide 16x16", 1, 20, 131072), ("wide 16x16", 9, 33, 70001), ("wide 16x32", 17, 20, 66000), ("wide 32x32", 17, 4000, 66000), ("wide 32x64", 40, 6000, 66000),
+        ("wide 64x64", 70, 4000, 66000), ("tile 128x128", 260, 6000, 66000), ("tile 64x128", 400, 4000, 66000), ("tile 128x256", 520, 8000, 66000), ("wide 16x32", 1030, 20, 66000)]
+
+
+@pytest.mark.parametrize("kernel,M,N,K", LONG)
+def test_linear_of_long_varied_rows(api, kernel, M, N, K):
+    # whole numbers below 2^53: the 64-bit product of the codes is exact wherever it runs, and in any order
+    assert kernel_of(api, M, N, K) == kernel
+    X, W = normal(M + K, (M, K), torch.bfloat16), normal(N + K, (N, K), torch.float16, 0.02)
+    Y = api.w8a8_gemm(X.cuda(), api.pack_w8(W.cuda()))
+    (xq, xs), (wq, ws) = oracle.quantize_rows(X.float().numpy()), oracle.quantize_rows(W.float().numpy())
+    acc = torch.zeros((M, N), dtype=torch.float64, device="cuda")
+    for k in range(0, K, 16384):
+        acc += torch.from_numpy(xq[:, k:k + 16384]).cuda().double() @ torch.from_numpy(wq[:, k:k + 16384]).cuda().double().t()
+    ref = acc.cpu().numpy() * xs.astype(np.float64)[:, None] * ws.astype(np.float64)[None, :]
+    tol = np.abs(ref) * (U[torch.bfloat16] + 4 * V) + 1e-37
+    assert (np.abs(f64(Y) - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("M", [1, 16, 200, 1100, 3000])
+@pytest.mark.parametrize("K", [1, 100, 5000, 20000])
+def test_rows_quantized_at_every_width_count_in_every_column(api, M, K):
+    # two features whose weights vary over all columns
+    X, W = normal(M + K, (M, K), torch.float16), normal(3 * K, (2, K), torch.float32)
+    check_linear(api.w8a8_gemm(X.cuda(), api.pack_w8(W.cuda())), X, W)
+
+
+@pytest.mark.parametrize("T", [2, 40, 300])
+@pytest.mark.parametrize("H,F", [(70001, 48), (40, 70001), (64, 131072)])
+def test_layer_of_long_rows(api, T, H, F):
+    layer, host = make_layer(api, H, F, 2, seed=T + H, std=0.02)
+    X = normal(T, (T, H), torch.float16, 0.2)
+    ids, gates = routing(T, 2, 1, seed=T)
+    check_layer(layer.forward(X.cuda(), ids.cuda(), gates.cuda()), X, host, ids, gates)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 100, 4096), (16, 64, 14336), (40, 300, 1000), (300, 1000, 640), (2000, 4000, 300)])
+def test_linear_of_the_largest_values(api, M, N, K):
+    # K times the largest magnitude next to 2^120, brought back by the weights, one of whose rows is all of its largest value
+    X, W = normal(M, (M, K), torch.float32), normal(N, (N, K), torch.float32)
+    X = (X / X.abs().max() * (2.0 ** 120 / K * 0.99)).to(torch.bfloat16)
+    X[0] = X.abs().max()
+    W[0] = W.abs().max()
+    W = W * 2.0 ** -100
+    check_linear(api.w8a8_gemm(X.cuda(), api.pack_w8(W.cuda())), X, W)
+
+
 # ---- router ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", DTYPES)
