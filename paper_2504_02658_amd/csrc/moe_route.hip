@@ -254,7 +254,10 @@ static int launch_gate_tile(const GateArgs& a, hipStream_t stream) {
 }
 template <int IN>
 static int launch_gate(const GateArgs& a, hipStream_t stream) {
-    // Both sides at 64 experts of 2048: 1024 tokens 31.8 and 30.2 us, 512 18.2 and 30, 4096 103 and 32.
+    // A workgroup per token reads the weight once per token, 16 tokens share it.  Both sides, us, at 512, 1024 and 4096 tokens: 64 experts of 2048 18, 31, 108
+    // and 30, 30, 31; 8 of 4096 12, 21, 77 and 18, 18, 20; 64 of 512 11, 18, 56 and 16; 128 of 4096 54, 99, 340 and 93; 256 of 7168 160, 301, 1099 and
+    // 290: they meet between 750 and 1050 tokens.  More than 256 experts have no room for their logits beside each other: 512 of 2048, 4096
+    // tokens, 769.
     if (a.T > 1024 && a.E <= kGateTileExperts) return a.E <= 16 ? launch_gate_tile<IN, 1>(a, stream) : launch_gate_tile<IN, 4>(a, stream);
     moe_gate_token_kernel<IN><<<dim3((unsigned)a.T), dim3(kGateThreads), 0, stream>>>(a);
     return launch_status();

@@ -394,8 +394,9 @@ static int launch_w8_tile(const W8TileArgs& a, int epi, W8Kernel k, hipStream_t 
     if (epi == 0) return a.act_bf16 ? launch_linear_tile<true>(a, k, stream) : launch_linear_tile<false>(a, k, stream);
     if (k != W8_TILE_128x256) return MILO_ERR_SHAPE;        // (experts: these rows alone)
     if (epi == 1) return launch_tile<2, 4, 1, 2, 2, 3, 1, false>(a, stream);
-    // Tiles that are half as wide where the wide ones would leave half of the compute units without one (45 tokens of 17 experts of 2730 x 1000: 49.6 us
-    // against 54.4 for the layer; where they fill the chip they cost more: 512 tokens of 8 of 14336 x 4096 473 against 448).
+    // Tiles that are half as wide where the wide ones would leave half of the compute units without one.  The layer, us: 45 tokens of 17 experts of
+    // 2730 x 1000, 76 wide tiles, 50.8 against 55.6; 512 of 8 of 4096 x 2048, 128 of them, 80 against 90; where they fill the chip they cost
+    // more: 512 of 8 of 14336 x 4096, 256 of them, 451 against 419.
     if ((int64_t)a.m_tiles * ((a.N + 255) / 256) <= device_cus() / 2)
         return launch_tile<2, 4, 1, 2, 1, 4, 2, false>(a, stream);
     return launch_tile<2, 4, 1, 2, 2, 3, 2, false>(a, stream);

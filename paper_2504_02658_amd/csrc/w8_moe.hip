@@ -76,8 +76,8 @@ __device__ __forceinline__ int slot_of(const int32_t* s_ids, int topk, int t, in
 // fragment, and have the next run on its way.  No branch stands between the loads: what lies past an end is loaded from a
 // clamped place and multiplied with zeros.  STAGED: the codes of the rows fit LDS, and the workgroup forms them there (so the
 // layer takes two launches); else a launch of the row quantizer has formed them (every workgroup reads all of its rows, so the
-// saving grows with the tokens).  Measured: 16 tokens to 8 experts of 14336 x 4096 read 940 MB in 167 us and 470 MB in 84 us, 5.6 TB/s;
-// one token to 8 of 1408 x 2048 46 MB in 12.8 us and 23 MB in 12.1 us, where the trips to memory one after another (ids, table,
+// saving grows with the tokens).  Measured: 16 tokens to 8 experts of 14336 x 4096 read 940 MB in 164 us and 470 MB in 83 us, 5.7 TB/s;
+// one token to 8 of 1408 x 2048 46 MB in 13.0 us and 23 MB in 11.9 us, where the trips to memory one after another (ids, table,
 // activations, weights) count.
 constexpr int kFewUpRun = 2, kFewDownRun = 4;
 
@@ -407,7 +407,8 @@ __global__ __launch_bounds__(256) void w8_combine_kernel(const float* __restrict
 // rows fastest the workgroups that do work then land on every second place that the dispatcher deals out, which it does in turn,
 // and half of the compute units idle.  Runs of eight columns keep an XCD's places even and its tiles of one expert close enough to share the weight; groups
 // of many slots spread every expert over all XCDs.  8 experts of 14336 x 4096: gate and up at 128 rows each 281 us with the rows
-// fastest in groups of 8, 203 so; 512 tokens 480 and 447 for the layer, 64 tokens 309 and 299; 4096 tokens of 66 x 1408 x 2048 577 and 545.
+// fastest in groups of 8, 203 so; the layer at 512 tokens 457 and 419, with 128 rows each 457 and 377, at 64 tokens 327 and 265; 4096 tokens
+// of 66 x 1408 x 2048 585 and 546.
 constexpr int kGroupM = 64, kSpan = 8;
 
 // Workspace of a forward.
@@ -433,9 +434,15 @@ static bool w8_moe_layout(int64_t T, int64_t H, int64_t F, int E, int topk, W8Mo
         return at;
     };
     L->few = T <= kFewTokens && P <= kFewMaxPairs;
-    // Rows per expert decide: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on their way soonest.  In those and in tiles of
-    // 128 x 256, us: 8 experts of 14336 x 4096, 10 rows each 260 and 293, 16 rows 268 and 296, 24 rows 288 and 305; 66 of 1408 x 2048, 8 rows 135 and
-    // 143, 19 rows 151 and 153, 31 rows 169 and 161.
+    // Rows per expert decide, on average, as the host knows no other number: the weights' bytes bound a few of them, and tiles of 32 x 64 have them on
+    // their way soonest.  In those and in tiles of 128 x 256, us, ids of equal popularity / popularity falling with the rank (the most popular expert has
+    // three to eight times the mean):
+    //   8 experts of 14336 x 4096    12 rows 257 and 290 / 263 and 287    20: 272 and 297 / 292 and 309    32: 323 and 305 / 333 and 332
+    //   66 of 1408 x 2048, 2 shared  12 rows 139 and 143 / 112 and 112    20: 150 and 149 / 132 and 127    32: 166 and 155 / 160 and 139
+    //   32 of 4096 x 1024            12 rows 108 and 108 /  95 and  99    20: 114 and 110 / 111 and 111    32: 135 and 114 / 142 and 122
+    //   17 of 2730 x 1000, 1 shared  12 rows  49 and  49 /  49 and  50    20:  52 and  55 /  53 and  55    32:  57 and  59 /  60 and  60
+    // Just below 24 rows the small tiles cost up to 11 % more than the large ones (24 rows of 66 experts: 157 and 151 / 144 and 130), just above it the large ones up to
+    // 5 % (8 experts: 285 and 300 / 304 and 318).
     L->kernel = P < 24 * (P < E ? P : E) ? W8_WIDE_32x64 : W8_TILE_128x256;
     // The grid has workgroups for every slot of the list of tiles, some of them empty.  Where those of the small tiles are too many (thousands of
     // experts of long rows), the large ones, which are a quarter as many, serve; where those are, the call is refused before it launches anything.
