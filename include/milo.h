@@ -379,8 +379,9 @@ int milo_moe_w3lr_routing_status(const void* workspace, void* stream);
  * and the linear is
  *     Y[m,n] = (sum over k of code_x[m,k] code_w[n,k]) * scale_x[m] * scale_w[n]
  * with the sum exact in 32-bit integers (whatever the order), its products with the scales in fp32, scale_x first, and one
- * rounding to the output type (bfloat16 activations: within fp32's range while K times their largest magnitude is below 2^120).  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale
- * NaN, so that what is computed from it is NaN and nothing else is touched.
+ * rounding to the output type.  (bfloat16 activations: within fp32's range while K times their largest magnitude is below
+ * 2^120.)  A row whose scale is zero or subnormal in fp32 stands for zeros; one with an infinity or a NaN has the scale NaN, so
+ * that what is computed from it is NaN and nothing else is touched.
  * Shapes: any N, K, M >= 1 up to K <= 131072 (the 32-bit sums), N, M < 2^22, N K, M K and M N <= 2^36; nothing has to
  * be a multiple of anything.  Pointers are 16-byte aligned, arrays dense.  These calls need no prepared workspace: theirs is scratch
  * alone, may hold anything before and after, and keeps nothing between calls; no kernel of theirs waits for another workgroup,
@@ -451,8 +452,11 @@ int milo_moe_w8a8_check_experts(const milo_w8_expert* experts, int E, int64_t H,
  *   workspace    milo_moe_w8a8_workspace(T, H, F, E, topk) bytes (0 if the shape is invalid), scratch
  * An id outside 0..E-1 contributes nothing; an expert without
  * tokens is legal, and a token without any gets zeros.  Two runs give bit-identical results.
- * Limits: as the linear's for [F x H] and [H x F]; T < 2^23, E max(H, F) <= 2^27, (T topk / 128 + 1 + E) (max(F / 128, H / 256) + 1) <= 2^22 (more
- * may pass; milo_moe_w8a8_workspace says so); the codes of T rows of H and of T topk rows of F within 4 GiB each.  A routed pair's weighted output stays fp32 until it is added to its token's sum, whose rounding to the output type is the only one.
+ * A routed pair's weighted output stays fp32 until it is added to its token's sum, whose rounding to the output type is the
+ * only one; so a token's result does not depend on the other tokens of the call, beyond the rounding of fp32.
+ * Limits: as the linear's for [F x H] and [H x F]; T < 2^23, E max(H, F) <= 2^27; the codes of T rows of H and of T topk rows of
+ * F within 4 GiB each; (T topk / 128 + 1 + E) (max(F / 128, H / 256) + 1) <= 2^22 (somewhat more may pass: the workspace's size
+ * is 0 for what does not).
  * Errors: NULL, SHAPE (also unknown flags), WORKSPACE, ALIGN, HIP.
  */
 size_t milo_moe_w8a8_workspace(int64_t T, int64_t H, int64_t F, int E, int topk);

@@ -114,6 +114,27 @@ def test_layer_codes_of_swiglu_rows_at_ties(api, T):
         assert np.array_equal(np.rint(got), want[t % len(S)]), (t, S[t % len(S)])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_layer_results_do_not_depend_on_the_other_tokens(api, dtype):
+    # One token alone, 13, 45 and 2100 of them take different kernels.  Codes are the same in all; a term carries at most five roundings of fp32, the
+    # sum of eight seven more: 12 v of the terms' magnitudes on either side, and the output's rounding.
+    T, H, F, E, topk = 2100, 1001, 300, 10, 8
+    layer, host = make_layer(api, H, F, E, seed=25)
+    X = normal(25, (T, H), dtype)
+    ids, gates = routing(T, E, topk, seed=26)
+    run = lambda rows: f64(layer.forward(X[rows].contiguous().cuda(), ids[rows].contiguous().cuda(), gates[rows].contiguous().cuda()))
+    whole = run(slice(0, T))
+    for first, n in ((0, 1), (2099, 1), (700, 13), (40, 16), (1000, 45), (1500, 300)):
+        rows = slice(first, first + n)
+        part = run(rows)
+        terms = oracle.w8a8_moe(X[rows].float().numpy(), host, ids[rows].numpy(), gates[rows].numpy())[2]
+        # (a rounding may fall on either side of a border: one step, 2 u, of the larger)
+        tol = 24 * V * terms + 2 * U[dtype] * (np.maximum(np.abs(part), np.abs(whole[rows])) + 24 * V * terms) + 2.0 ** -24
+        assert (np.abs(part - whole[rows]) <= tol).all()
+        # (sums that far apart round to other outputs with the probability 24 v / 2 u of the terms over the output, fp16 0.2 % of some three)
+        assert (part != whole[rows]).mean() < 0.02
+
+
 @pytest.mark.parametrize("T", [2, 20, 300])
 def test_layer_down_sums_that_cancel(api, T):
     # The second half of the features is the first half with the down projection's sign turned: every integer sum is zero, whatever
